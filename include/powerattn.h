@@ -344,6 +344,152 @@ pa_status pa_kv_append(const pa_paged_params *p, const void *k_new, const void *
                        int32_t *cache_lens, void *stream);
 
 /* ------------------------------------------------------------------------------------------
+ * Block tables: which page and slot every new token of a batch goes to.  (The paper decodes behind a
+ * long input, Section 4.5, and says nothing about where the cache lies; this serves the paged caches.)
+ *
+ * A sequence b holds cache_lens[b] = c tokens in ceil(c / 64) pages, block_table[b, 0 ..], and gets
+ * new_lens[b] = n more.  The pages it still needs are taken from a stack, free_pages[0 .. *free_count - 1],
+ * from its top downwards: sequence after sequence, block after block.
+ *   - A sequence is refused if c or n is negative, if it would need more than max_blocks_per_seq pages, if
+ *     its tokens would end behind max_tokens (all three: it takes no part in the count of pages either), or
+ *     if the stack does not hold the pages of all sequences up to and including it (one that needs no page
+ *     is served all the same).  Nothing of it changes: no page, lens_out = c, its slots -1.
+ *   - The new tokens are packed, refused ones included: cu_seqlens[b] counts those before sequence b (a
+ *     negative n counts as 0; sums beyond 2^31 - 1 are held at that).  Token cu_seqlens[b] + i has
+ *     positions[...] = c + i and slot_map[...] = 64 page + (c + i) mod 64, the page being block_table[b,
+ *     (c + i) / 64], or -1 where that page lies outside [0, n_pages).
+ *   - Tokens from cu_seqlens[batch] up to max_tokens have slot and position -1 (a padded batch).
+ * lens_out[b] = c + n for a sequence that is served; *free_left is what the stack still holds.  The table's
+ * other entries stay as they are.
+ * ------------------------------------------------------------------------------------------ */
+typedef struct {
+    int32_t batch;              /* sequences, <= 65535                                  */
+    int32_t block;              /* page size in tokens, must be 64                      */
+    int32_t max_blocks_per_seq; /* row length of block_table                            */
+    int32_t n_pages;            /* pages in the pool                                    */
+    int32_t max_tokens;         /* entries of slot_map and positions                    */
+    int32_t free_capacity;      /* entries of free_pages; a larger *free_count is cut   */
+} pa_table_params;
+
+/* Bytes of device scratch (16-byte aligned start): what the sequences need, from one kernel to the next. */
+size_t pa_build_block_tables_workspace_bytes(const pa_table_params *p);
+
+/* All pointers are device memory: new_lens, cache_lens, lens_out int32 [batch]; free_pages int32
+ * [free_capacity]; free_count, free_left int32 [1]; block_table int32 [batch, max_blocks_per_seq], read
+ * and written; cu_seqlens int32 [batch + 1]; slot_map int64 [max_tokens]; positions int32 [max_tokens].
+ * lens_out may be cache_lens and free_left may be free_count; no other two may overlap.  One kernel is
+ * enqueued for small batches, else two.  Calls that share a workspace must not overlap on the GPU.
+ * Errors: PA_ERR_INVALID_ARG, PA_ERR_SHAPE, PA_ERR_ALIGNMENT, PA_ERR_WORKSPACE, PA_ERR_CUDA. */
+pa_status pa_build_block_tables(const pa_table_params *p, const int32_t *new_lens, const int32_t *cache_lens,
+                                const int32_t *free_pages, const int32_t *free_count, int32_t *block_table,
+                                int32_t *cu_seqlens, int64_t *slot_map, int32_t *positions, int32_t *lens_out,
+                                int32_t *free_left, void *workspace, size_t workspace_bytes, void *stream);
+
+/* ------------------------------------------------------------------------------------------
+ * Queries and keys before the attention: the root-mean-square norm of each head and the rotation by the
+ * token's position, in one pass over both.  For a head x of head_dim = D features at position pos:
+ *   r = 1 / sqrt(mean_i x_i^2 + eps);   y_i = x_i r w_i;
+ *   (out_a, out_b) = (y_a cos - y_b sin, y_b cos + y_a sin)
+ * for the pairs (a, b) = (i, i + rotary_dim / 2), or (2 i, 2 i + 1) if interleaved, i < rotary_dim / 2, with
+ * cos = cos_sin[pos, i], sin = cos_sin[pos, rotary_dim / 2 + i]; the features from rotary_dim on are y_i.
+ * Arithmetic in fp32, outputs rounded to bf16.  A token whose position lies outside [0, max_positions)
+ * is left alone: its rows of the outputs keep what they hold.
+ * ------------------------------------------------------------------------------------------ */
+typedef struct {
+    int32_t batch, n_q_heads, n_kv_heads, head_dim; /* head_dim in {64, 128}                   */
+    int64_t seq_len;                                /* tokens of a batch entry                 */
+    int32_t rotary_dim;                             /* a multiple of 8, in [0, head_dim]       */
+    int32_t interleaved;                            /* 0: pairs (i, i + rotary_dim / 2)        */
+    int32_t max_positions;                          /* rows of cos_sin                         */
+    float eps;                                      /* >= 0                                    */
+    pa_dtype w_dtype;                               /* of both weights                         */
+    pa_strides q, k, q_out, k_out;                  /* [batch, seq_len, heads, head_dim]       */
+} pa_rope_params;
+
+/* q, k, q_out, k_out: device bf16 by strides; q_out may be q and k_out may be k, with the same strides.
+ * q_weight, k_weight: device, w_dtype [head_dim].  cos_sin: device fp32 [max_positions, rotary_dim].
+ * positions: device int32 [batch, seq_len].  One kernel is enqueued. */
+pa_status pa_qk_norm_rope(const pa_rope_params *p, const void *q, const void *k, const void *q_weight,
+                          const void *k_weight, const float *cos_sin, const int32_t *positions, void *q_out,
+                          void *k_out, void *stream);
+
+/* The gradients.  With g the gradient d_out rotated back (by -angle), x^ = x r and h = g w:
+ *   dw_i = sum over tokens and heads of g_i x^_i;   dx = r (h - x^ mean_i(h_i x^_i)).
+ * p, q .. positions: as given to pa_qk_norm_rope, with the strides of d_q_out, d_k_out (d_dtype: bf16 or
+ * fp32, what pa_prefill_backward returns) in p->q_out and p->k_out.  dq, dk: device bf16 contiguous.
+ * dq_weight, dk_weight: device fp32 [head_dim], overwritten.  A token whose position lies outside the table
+ * has gradients 0 and adds nothing.  workspace: device, 16-byte aligned,
+ * >= pa_qk_norm_rope_backward_workspace_bytes(p).  Two kernels are enqueued; the sums over tokens are taken
+ * in a fixed order.  Calls that share a workspace must not overlap on the GPU. */
+size_t pa_qk_norm_rope_backward_workspace_bytes(const pa_rope_params *p);
+pa_status pa_qk_norm_rope_backward(const pa_rope_params *p, const void *q, const void *k, const void *q_weight,
+                                   const void *k_weight, const float *cos_sin, const int32_t *positions,
+                                   const void *d_q_out, const void *d_k_out, pa_dtype d_dtype, void *dq, void *dk,
+                                   float *dq_weight, float *dk_weight, void *workspace, size_t workspace_bytes,
+                                   void *stream);
+
+/* ------------------------------------------------------------------------------------------
+ * A paged KV cache in 4 bits: pages of 64 tokens as for pa_decode_paged, in 28 % of their bytes.
+ *
+ * A group is 32 consecutive features of one token and KV head, its values x_i bf16.  With a = max |x_i| the
+ * group's scale is s = a / 7 rounded to bf16 and n_i = x_i / s rounded to the nearest integer, ties towards
+ * zero: the cache stands for the values s n_i, n_i in -7 .. 7.  A group with a < 2^-100 is held as zeros, one
+ * with an infinity or NaN as NaNs.
+ *
+ * The pool is [n_pages, n_kv_heads] records of pa_kv4_page_bytes(head_dim) = 72 head_dim bytes by the two
+ * strides: 64 rows of K nibbles (n_i + 8, lower half of a byte first; head_dim / 2 bytes a token), 64 rows of
+ * K scales (bf16 [head_dim / 32]), then the same for V.  Inside a row the nibbles stand in the order in which
+ * pa_decode_kv4's tensor-core fragments take them.  With NG = head_dim / 32: in a K row the features 32 j +
+ * 8 t + (0 .. 7) are word t NG + j (t < 4).  A V row is 8 chunks of 4 NG nibbles; the features 32 j + 4 g +
+ * (0 .. 3) start at nibble 4 j of chunk g, or of chunk g ^ 4 in tokens with (token & 2) set.
+ * ------------------------------------------------------------------------------------------ */
+typedef struct {
+    int32_t n_kv_heads, head_dim;     /* head_dim in {64, 128}                                   */
+    int32_t block;                    /* tokens of a page, must be 64                            */
+    int32_t n_pages;                  /* pages in the pool                                       */
+    int64_t page_stride, head_stride; /* in BYTES, multiples of 16                               */
+} pa_kv4_pool;
+
+/* Bytes of a page and KV head; 0 if head_dim is neither 64 nor 128. */
+size_t pa_kv4_page_bytes(int32_t head_dim);
+
+/* Writes tokens to their slots: token i goes to page slot_map[i] / 64, place slot_map[i] mod 64 (device int64
+ * [n_tokens]; pa_build_block_tables makes it).  A slot outside [0, 64 n_pages) is skipped.  k_new, v_new:
+ * device bf16 [n_tokens, n_kv_heads, head_dim] by their .seq and .head strides.  The slots of a call differ
+ * from one another (one that is given twice holds a mixture).  One kernel is enqueued. */
+pa_status pa_kv4_append(const pa_kv4_pool *pool, int64_t n_tokens, const void *k_new, const void *v_new,
+                        pa_strides k_strides, pa_strides v_strides, void *kv_pool, const int64_t *slot_map,
+                        void *stream);
+
+/* The values that slots hold: k_out, v_out device [n_tokens, n_kv_heads, head_dim] contiguous, dtype (fp32
+ * exact, bf16 rounded).  A slot outside the pool reads as zeros.  One kernel is enqueued. */
+pa_status pa_kv4_read(const pa_kv4_pool *pool, int64_t n_tokens, const void *kv_pool, const int64_t *slot_map,
+                      void *k_out, void *v_out, pa_dtype dtype, void *stream);
+
+typedef struct {
+    int32_t batch, n_q_heads;           /* at most 8 query heads per KV head               */
+    int32_t window_blocks, sink_blocks;
+    int32_t max_blocks_per_seq;         /* row length of block_table                       */
+    float softmax_scale;                /* 0 => 1 / sqrt(head_dim)                         */
+    pa_dtype o_dtype;
+    pa_kv4_pool pool;
+} pa_kv4_params;
+
+size_t pa_decode_kv4_workspace_bytes(const pa_kv4_params *p);
+
+/* As pa_decode_paged (the same row of the mask, block_table, cache_lens, outputs, and pa_decode_status on the
+ * workspace), on a 4-bit pool.  Logits are sums of exact products in fp32.  The weights, times V's scales, are
+ * rounded to bf16 for bf16 outputs and held in two bf16 parts for fp32 outputs.
+ * workspace: device, 16-byte aligned, >= pa_decode_kv4_workspace_bytes(p); calls that share one must not
+ * overlap on the GPU.  A table entry outside [0, n_pages) is clamped into the pool; the sequence's result is
+ * then meaningless.  One kernel is enqueued, or two where rows are few and long (their parts are merged by the
+ * second).  PA_DECODE_CLUSTER=n (1..8) sets the CTAs per row, PA_DECODE_PATH=cluster / =persist / =splitk the
+ * form of the kernel (see pa_decode). */
+pa_status pa_decode_kv4(const pa_kv4_params *p, const void *q, const void *kv_pool, const int32_t *block_table,
+                        const int32_t *cache_lens, void *o, float *lse, void *workspace, size_t workspace_bytes,
+                        void *stream);
+
+/* ------------------------------------------------------------------------------------------
  * Decode without any allocation.  (The paper has no counterpart to this entry point; it exists
  * for integration reasons only.)
  *

@@ -29,7 +29,9 @@ EXPORTS = ["pa_status_string", "pa_last_error_message", "pa_version", "pa_reload
            "pa_prefill_backward_workspace_bytes", "pa_prefill_backward",
            "pa_decode_workspace_bytes", "pa_decode", "pa_decode_status", "pa_decode_block_list",
            "pa_decode_row_block_set", "pa_decode_paged_workspace_bytes", "pa_decode_paged", "pa_kv_append",
-           "pa_decode_static"]
+           "pa_decode_static", "pa_build_block_tables_workspace_bytes", "pa_build_block_tables", "pa_qk_norm_rope",
+           "pa_qk_norm_rope_backward_workspace_bytes", "pa_qk_norm_rope_backward", "pa_kv4_page_bytes", "pa_kv4_append",
+           "pa_kv4_read", "pa_decode_kv4_workspace_bytes", "pa_decode_kv4"]
 
 
 class PaError(RuntimeError):
@@ -64,6 +66,30 @@ class pa_paged_params(ctypes.Structure):
                 ("sink_blocks", ctypes.c_int32), ("n_pages", ctypes.c_int32),
                 ("max_blocks_per_seq", ctypes.c_int32), ("softmax_scale", ctypes.c_float),
                 ("k", pa_strides), ("v", pa_strides), ("o_dtype", ctypes.c_int)]
+
+
+class pa_table_params(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("block", ctypes.c_int32), ("max_blocks_per_seq", ctypes.c_int32),
+                ("n_pages", ctypes.c_int32), ("max_tokens", ctypes.c_int32), ("free_capacity", ctypes.c_int32)]
+
+
+class pa_rope_params(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("n_q_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("seq_len", ctypes.c_int64), ("rotary_dim", ctypes.c_int32),
+                ("interleaved", ctypes.c_int32), ("max_positions", ctypes.c_int32), ("eps", ctypes.c_float),
+                ("w_dtype", ctypes.c_int), ("q", pa_strides), ("k", pa_strides), ("q_out", pa_strides),
+                ("k_out", pa_strides)]
+
+
+class pa_kv4_pool(ctypes.Structure):
+    _fields_ = [("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("block", ctypes.c_int32),
+                ("n_pages", ctypes.c_int32), ("page_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+
+
+class pa_kv4_params(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("n_q_heads", ctypes.c_int32), ("window_blocks", ctypes.c_int32),
+                ("sink_blocks", ctypes.c_int32), ("max_blocks_per_seq", ctypes.c_int32),
+                ("softmax_scale", ctypes.c_float), ("o_dtype", ctypes.c_int), ("pool", pa_kv4_pool)]
 
 
 def _load() -> ctypes.CDLL:
@@ -130,6 +156,25 @@ def _load() -> ctypes.CDLL:
                                     ctypes.c_size_t, vp]
     lib.pa_kv_append.restype = ctypes.c_int
     lib.pa_kv_append.argtypes = [ctypes.POINTER(pa_paged_params), vp, vp, vp, vp, vp, vp, vp]
+    for name, params in (("pa_build_block_tables", pa_table_params), ("pa_qk_norm_rope_backward", pa_rope_params),
+                         ("pa_decode_kv4", pa_kv4_params)):
+        size_of = getattr(lib, name + "_workspace_bytes")
+        size_of.restype, size_of.argtypes = ctypes.c_size_t, [ctypes.POINTER(params)]
+    size = ctypes.c_size_t
+    lib.pa_build_block_tables.restype = ctypes.c_int
+    lib.pa_build_block_tables.argtypes = [ctypes.POINTER(pa_table_params)] + [vp] * 11 + [size, vp]
+    lib.pa_qk_norm_rope.restype = ctypes.c_int
+    lib.pa_qk_norm_rope.argtypes = [ctypes.POINTER(pa_rope_params)] + [vp] * 9
+    lib.pa_qk_norm_rope_backward.restype = ctypes.c_int
+    lib.pa_qk_norm_rope_backward.argtypes = ([ctypes.POINTER(pa_rope_params)] + [vp] * 8 + [ctypes.c_int] + [vp] * 5 +
+                                             [size, vp])
+    lib.pa_kv4_page_bytes.restype, lib.pa_kv4_page_bytes.argtypes = size, [i32]
+    lib.pa_kv4_append.restype = ctypes.c_int
+    lib.pa_kv4_append.argtypes = [ctypes.POINTER(pa_kv4_pool), i64, vp, vp, pa_strides, pa_strides, vp, vp, vp]
+    lib.pa_kv4_read.restype = ctypes.c_int
+    lib.pa_kv4_read.argtypes = [ctypes.POINTER(pa_kv4_pool), i64, vp, vp, vp, vp, ctypes.c_int, vp]
+    lib.pa_decode_kv4.restype = ctypes.c_int
+    lib.pa_decode_kv4.argtypes = [ctypes.POINTER(pa_kv4_params)] + [vp] * 7 + [size, vp]
     return lib
 
 
@@ -350,6 +395,71 @@ def pa_decode_paged(q, k_pool, v_pool, block_table, cache_lens, window_blocks: i
 def pa_kv_append(k_new, v_new, k_pool, v_pool, block_table, cache_lens, block: int = 64) -> None:
     """k_new, v_new [batch, Hkv, D] go to position cache_lens[b] of each sequence; cache_lens grows by one."""
     _calls.kv_append(k_new, v_new, k_pool, v_pool, block_table, cache_lens, block)
+
+
+def pa_build_block_tables(new_lens, cache_lens, free_pages, free_count, block_table, n_pages: int, max_tokens: int,
+                          cu_seqlens=None, slot_map=None, positions=None, lens_out=None, free_left=None, workspace=None,
+                          block: int = 64):
+    """Pages, slots and positions for new_lens[b] more tokens behind each sequence's cache_lens[b]: int32 device
+    tensors [batch], a stack of free pages and its height free_count [1], block_table int32 [batch, max_blocks]
+    (its new entries are written).  lens_out may be cache_lens and free_left may be free_count.
+    Returns (cu_seqlens int32 [batch + 1], slot_map int64 [max_tokens], positions int32 [max_tokens], lens_out,
+    free_left, workspace)."""
+    return _calls.build_block_tables(new_lens, cache_lens, free_pages, free_count, block_table, n_pages, max_tokens,
+                                     cu_seqlens, slot_map, positions, lens_out, free_left, workspace, block)
+
+
+def pa_qk_norm_rope(q, k, q_weight, k_weight, cos_sin, positions, q_out=None, k_out=None, eps: float = 1e-6,
+                    interleaved: bool = False):
+    """Norm of each head and rotation by position: q [tokens, Hq, D], k [tokens, Hkv, D] bf16 (or [batch, N, H, D];
+    any strides with contiguous features), weights [D], cos_sin fp32 [positions, rotary_dim] (cosines, then sines),
+    positions int32, one a token.  Returns (q_out, k_out), which may be q and k; rows of tokens whose position is
+    outside the table are not written."""
+    return _calls.qk_norm_rope(q, k, q_weight, k_weight, cos_sin, positions, q_out, k_out, eps, interleaved)
+
+
+def pa_qk_norm_rope_backward(q, k, q_weight, k_weight, cos_sin, positions, d_q_out, d_k_out, dq=None, dk=None,
+                             dq_weight=None, dk_weight=None, workspace=None, eps: float = 1e-6,
+                             interleaved: bool = False):
+    """Gradients of pa_qk_norm_rope; d_q_out, d_k_out bf16 or fp32.  Returns (dq, dk, dq_weight, dk_weight,
+    workspace): bf16 contiguous, the weights' fp32."""
+    return _calls.qk_norm_rope_backward(q, k, q_weight, k_weight, cos_sin, positions, d_q_out, d_k_out, dq, dk, dq_weight,
+                                        dk_weight, workspace, eps, interleaved)
+
+
+def pa_kv4_page_bytes(head_dim: int) -> int:
+    """Bytes of a page and KV head of the 4-bit cache, the last axis of its pool."""
+    return int(lib.pa_kv4_page_bytes(head_dim))
+
+
+def pa_kv4_append(k_new, v_new, kv_pool, slot_map) -> None:
+    """k_new, v_new bf16 [tokens, Hkv, D] go to the slots slot_map (int64, one a token) of kv_pool, uint8
+    [n_pages, Hkv, pa_kv4_page_bytes(D)]; tokens whose slot is outside the pool are skipped."""
+    _calls.kv4_append(k_new, v_new, kv_pool, slot_map)
+
+
+def pa_kv4_read(kv_pool, slot_map, head_dim: int, k_out=None, v_out=None, dtype=torch.bfloat16):
+    """The values that slots hold.  Returns (k, v) [tokens, Hkv, D], zeros for slots outside the pool."""
+    return _calls.kv4_read(kv_pool, slot_map, head_dim, k_out, v_out, dtype)
+
+
+def kv4_params(q, kv_pool, block_table, window_blocks: int, sink_blocks: int, softmax_scale: float = 0.0,
+               o_dtype=torch.bfloat16) -> pa_kv4_params:
+    batch, hq, d = q.shape
+    pool = pa_kv4_pool(kv_pool.shape[1], d, 64, kv_pool.shape[0], kv_pool.stride(0), kv_pool.stride(1))
+    return pa_kv4_params(batch, hq, window_blocks, sink_blocks, block_table.shape[1], float(softmax_scale),
+                         PA_F32 if o_dtype == torch.float32 else PA_BF16, pool)
+
+
+def pa_decode_kv4_workspace_bytes(params: pa_kv4_params) -> int:
+    return int(lib.pa_decode_kv4_workspace_bytes(ctypes.byref(params)))
+
+
+def pa_decode_kv4(q, kv_pool, block_table, cache_lens, window_blocks: int, sink_blocks: int, o=None, lse=None,
+                  workspace=None, softmax_scale: float = 0.0, o_dtype=torch.bfloat16):
+    """pa_decode_paged on a 4-bit pool (see pa_kv4_append).  Returns (o, lse, workspace)."""
+    return _calls.decode_kv4(q, kv_pool, block_table, cache_lens, window_blocks, sink_blocks, o, lse, workspace,
+                             softmax_scale, o_dtype)
 
 
 PA_DECODE_STATIC_SCRATCH_BYTES = 4 << 20

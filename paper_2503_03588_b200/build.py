@@ -16,7 +16,8 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libpowerattn.so")
 CALLS = os.path.join(PKG, "_calls.so")
 CALLS_STAMP = os.path.join(PKG, "_calls.stamp")  # what _calls.so was built against
-SOURCES = ["api.cu", "layout.cu", "decode.cu", "prefill_sm100.cu", "backward.cu", "backward_sm100.cu"]
+SOURCES = ["api.cu", "layout.cu", "decode.cu", "prefill_sm100.cu", "backward.cu", "backward_sm100.cu", "tables.cu",
+           "qk_norm_rope.cu", "kv4_cache.cu", "kv4_decode.cu"]
 
 
 def _nvcc() -> str:

@@ -9,6 +9,7 @@
 
 #include <ATen/ops/empty.h>
 #include <c10/core/DefaultDtype.h>
+#include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Device.h>
 #include <torch/csrc/Dtype.h>
@@ -133,7 +134,8 @@ void run(Call call)
 template <typename... O>
 PyObject *tuple(const O &...outs)
 {
-    return Py_BuildValue(sizeof...(O) == 3 ? "(NNN)" : "(NNNN)", outs.object()...);
+    static const char *const formats[] = {"(NN)", "(NNN)", "(NNNN)", "(NNNNN)", "(NNNNNN)"};
+    return Py_BuildValue(formats[sizeof...(O) - 2], outs.object()...);
 }
 
 pa_prefill_params prefill_params(const at::Tensor &q, const at::Tensor &k, const at::Tensor &v, const at::Tensor &o,
@@ -335,6 +337,203 @@ PyObject *build_layout(PyObject *const *x)
     return Py_BuildValue("(NN)", row_ptr.object(), col_idx.object());
 }
 
+// Every tensor lies on the current CUDA device (whose stream the call goes to).
+template <typename... T>
+void on_current_device(const T &...tensors)
+{
+    for (const at::Tensor *t : {&tensors...})
+        expect(t->is_cuda() && t->get_device() == c10::cuda::current_device(), "expected tensors on the current CUDA device");
+}
+bool is_bf16(const at::Tensor &t) { return t.scalar_type() == at::kBFloat16; }
+bool is_f32(const at::Tensor &t) { return t.scalar_type() == at::kFloat; }
+bool plain(const at::Tensor &t, at::ScalarType type, at::IntArrayRef size)
+{
+    return t.scalar_type() == type && t.is_contiguous() && t.sizes() == size;
+}
+
+// new_lens, cache_lens, free_pages, free_count, block_table, n_pages, max_tokens, cu_seqlens, slot_map, positions, lens_out,
+// free_left, workspace, block
+PyObject *build_block_tables(PyObject *const *x)
+{
+    const at::Tensor &fresh = tensor(x[0]), &cached = tensor(x[1]), &pages = tensor(x[2]), &count = tensor(x[3]),
+                     &table = tensor(x[4]);
+    const int64_t batch = fresh.numel();
+    const int32_t n_pages = integer32(x[5]), max_tokens = integer32(x[6]), block = integer32(x[13]);
+    expect(plain(fresh, at::kInt, {batch}) && plain(cached, at::kInt, {batch}) && plain(pages, at::kInt, {pages.numel()}) &&
+               plain(count, at::kInt, {1}),
+           "expected contiguous int32 new_lens and cache_lens [batch], free_pages [n], free_count [1]");
+    expect(table.dim() == 2 && plain(table, at::kInt, {batch, table.size(1)}), "expected a contiguous int32 block table [batch, max_blocks]");
+    expect(table.size(1) <= INT32_MAX && pages.numel() <= INT32_MAX && batch <= INT32_MAX && max_tokens >= 0, "too large or negative a size");
+    on_current_device(fresh, cached, pages, count, table);
+    const Out cu(x[7], [&] { return make(fresh, {batch + 1}, at::kInt); });
+    const Out slots(x[8], [&] { return make(fresh, {max_tokens}, at::kLong); });
+    const Out positions(x[9], [&] { return make(fresh, {max_tokens}, at::kInt); });
+    const Out lens(x[10], [&] { return make(fresh, {batch}, at::kInt); });
+    const Out left(x[11], [&] { return make(fresh, {1}, at::kInt); });
+    const pa_table_params p = {(int32_t)batch, block, (int32_t)table.size(1), n_pages, max_tokens,
+                               (int32_t)pages.numel()};
+    const Out ws(x[12], [&] { return make_bytes(fresh, pa_build_block_tables_workspace_bytes(&p)); });
+    expect(plain(cu.t, at::kInt, {batch + 1}) && plain(slots.t, at::kLong, {max_tokens}) && plain(positions.t, at::kInt, {max_tokens}) &&
+               plain(lens.t, at::kInt, {batch}) && plain(left.t, at::kInt, {1}),
+           "expected contiguous int32 cu_seqlens [batch + 1], positions [max_tokens], lens_out [batch], free_left [1], int64 slot_map");
+    on_current_device(cu.t, slots.t, positions.t, lens.t, left.t, ws.t);
+    run([&] {
+        return pa_build_block_tables(&p, (const int32_t *)fresh.data_ptr(), (const int32_t *)cached.data_ptr(),
+                                     (const int32_t *)pages.data_ptr(), (const int32_t *)count.data_ptr(), (int32_t *)table.data_ptr(),
+                                     (int32_t *)cu.ptr(), (int64_t *)slots.ptr(), (int32_t *)positions.ptr(), (int32_t *)lens.ptr(),
+                                     (int32_t *)left.ptr(), ws.ptr(), (size_t)ws.t.nbytes(), stream());
+    });
+    return tuple(cu, slots, positions, lens, left, ws);
+}
+
+// Queries or keys [tokens, head, head_dim] or [batch, seq, head, head_dim].
+pa_strides token_strides(const at::Tensor &t)
+{
+    expect((t.dim() == 3 || t.dim() == 4) && t.stride(-1) == 1,
+           "expected [tokens, head, head_dim] or [batch, seq, head, head_dim] with contiguous head_dim");
+    return {t.dim() == 4 ? t.stride(0) : 0, t.stride(-3), t.stride(-2)};
+}
+pa_rope_params rope_params(const at::Tensor &q, const at::Tensor &k, const at::Tensor &wq, const at::Tensor &wk,
+                           const at::Tensor &cos_sin, const at::Tensor &positions, const at::Tensor &q_like, const at::Tensor &k_like,
+                           float eps, bool interleaved)
+{
+    const pa_strides sq = token_strides(q), sk = token_strides(k), sqo = token_strides(q_like), sko = token_strides(k_like);
+    const int64_t batch = q.dim() == 4 ? q.size(0) : 1, seq = q.size(-3), d = q.size(-1);
+    expect(is_bf16(q) && is_bf16(k), "q and k are bfloat16");
+    expect(k.dim() == q.dim() && (q.dim() == 3 || k.size(0) == batch) && k.size(-3) == seq && k.size(-1) == d &&
+               q_like.sizes() == q.sizes() && k_like.sizes() == k.sizes(),
+           "q and k, and what goes with them, have the same tokens and head_dim");
+    expect(wq.scalar_type() == wk.scalar_type() && (is_bf16(wq) || is_f32(wq)) && plain(wq, wq.scalar_type(), {d}) &&
+               plain(wk, wq.scalar_type(), {d}),
+           "the weights are [head_dim], both bfloat16 or both float32");
+    expect(cos_sin.dim() == 2 && is_f32(cos_sin) && cos_sin.is_contiguous(), "cos_sin is contiguous float32 [positions, rotary_dim]");
+    expect(is_int32(positions) && positions.is_contiguous() && positions.numel() == batch * seq, "positions is contiguous int32, one a token");
+    const int64_t most = cos_sin.size(0);
+    expect(batch <= INT32_MAX && q.size(-2) <= INT32_MAX && k.size(-2) <= INT32_MAX && d <= INT32_MAX && cos_sin.size(1) <= INT32_MAX,
+           "too large a size");
+    on_current_device(q, k, wq, wk, cos_sin, positions, q_like, k_like);
+    return {(int32_t)batch, (int32_t)q.size(-2), (int32_t)k.size(-2), (int32_t)d, seq, (int32_t)cos_sin.size(1), interleaved ? 1 : 0,
+            (int32_t)(most > INT32_MAX ? INT32_MAX : most), eps, is_f32(wq) ? PA_F32 : PA_BF16, sq, sk, sqo, sko};
+}
+bool truth(PyObject *o)
+{
+    const int v = PyObject_IsTrue(o);
+    if (v < 0) throw Raised();
+    return v != 0;
+}
+
+// q, k, q_weight, k_weight, cos_sin, positions, q_out, k_out, eps, interleaved
+PyObject *qk_norm_rope(PyObject *const *x)
+{
+    const at::Tensor &q = tensor(x[0]), &k = tensor(x[1]), &wq = tensor(x[2]), &wk = tensor(x[3]), &cos_sin = tensor(x[4]),
+                     &positions = tensor(x[5]);
+    const Out q_out(x[6], [&] { return make(q, q.sizes(), at::kBFloat16); });
+    const Out k_out(x[7], [&] { return make(k, k.sizes(), at::kBFloat16); });
+    expect(is_bf16(q_out.t) && is_bf16(k_out.t), "q_out and k_out are bfloat16");
+    const pa_rope_params p = rope_params(q, k, wq, wk, cos_sin, positions, q_out.t, k_out.t, number(x[8]), truth(x[9]));
+    run([&] {
+        return pa_qk_norm_rope(&p, q.data_ptr(), k.data_ptr(), wq.data_ptr(), wk.data_ptr(), (const float *)cos_sin.data_ptr(),
+                               (const int32_t *)positions.data_ptr(), q_out.ptr(), k_out.ptr(), stream());
+    });
+    return tuple(q_out, k_out);
+}
+
+// q, k, q_weight, k_weight, cos_sin, positions, d_q_out, d_k_out, dq, dk, dq_weight, dk_weight, workspace, eps, interleaved
+PyObject *qk_norm_rope_backward(PyObject *const *x)
+{
+    const at::Tensor &q = tensor(x[0]), &k = tensor(x[1]), &wq = tensor(x[2]), &wk = tensor(x[3]), &cos_sin = tensor(x[4]),
+                     &positions = tensor(x[5]), &d_q = tensor(x[6]), &d_k = tensor(x[7]);
+    expect(d_q.scalar_type() == d_k.scalar_type() && (is_bf16(d_q) || is_f32(d_q)),
+           "the gradients of the outputs are both bfloat16 or both float32");
+    const pa_rope_params p = rope_params(q, k, wq, wk, cos_sin, positions, d_q, d_k, number(x[13]), truth(x[14]));
+    const Out dq(x[8], [&] { return make(q, q.sizes(), at::kBFloat16); });
+    const Out dk(x[9], [&] { return make(k, k.sizes(), at::kBFloat16); });
+    const Out dwq(x[10], [&] { return make(q, {q.size(-1)}, at::kFloat); });
+    const Out dwk(x[11], [&] { return make(q, {q.size(-1)}, at::kFloat); });
+    const Out ws(x[12], [&] { return make_bytes(q, pa_qk_norm_rope_backward_workspace_bytes(&p)); });
+    expect(plain(dq.t, at::kBFloat16, q.sizes()) && plain(dk.t, at::kBFloat16, k.sizes()) && plain(dwq.t, at::kFloat, {q.size(-1)}) &&
+               plain(dwk.t, at::kFloat, {q.size(-1)}),
+           "dq and dk are contiguous bfloat16, the weights' gradients float32 [head_dim]");
+    on_current_device(dq.t, dk.t, dwq.t, dwk.t, ws.t);
+    run([&] {
+        return pa_qk_norm_rope_backward(&p, q.data_ptr(), k.data_ptr(), wq.data_ptr(), wk.data_ptr(), (const float *)cos_sin.data_ptr(),
+                                        (const int32_t *)positions.data_ptr(), d_q.data_ptr(), d_k.data_ptr(),
+                                        is_f32(d_q) ? PA_F32 : PA_BF16, dq.ptr(), dk.ptr(), (float *)dwq.ptr(), (float *)dwk.ptr(),
+                                        ws.ptr(), (size_t)ws.t.nbytes(), stream());
+    });
+    return tuple(dq, dk, dwq, dwk, ws);
+}
+
+pa_kv4_pool kv4_pool(const at::Tensor &pool, int64_t head_dim)
+{
+    expect(pool.dim() == 3 && pool.scalar_type() == at::kByte && pool.stride(2) == 1 && head_dim <= 128 &&
+               pool.size(2) == (int64_t)pa_kv4_page_bytes((int32_t)head_dim),
+           "expected a uint8 pool [n_pages, n_kv_heads, pa_kv4_page_bytes(head_dim)] with contiguous records");
+    expect(pool.size(0) <= INT32_MAX && pool.size(1) <= INT32_MAX, "too large a size");
+    return {(int32_t)pool.size(1), (int32_t)head_dim, 64, (int32_t)pool.size(0), pool.stride(0), pool.stride(1)};
+}
+
+// k_new, v_new, kv_pool, slot_map
+PyObject *kv4_append(PyObject *const *x)
+{
+    const at::Tensor &k = tensor(x[0]), &v = tensor(x[1]), &pool = tensor(x[2]), &slots = tensor(x[3]);
+    expect(k.dim() == 3 && v.sizes() == k.sizes() && is_bf16(k) && is_bf16(v) && k.stride(2) == 1 && v.stride(2) == 1,
+           "expected bfloat16 k_new and v_new [tokens, head, head_dim] with contiguous head_dim");
+    expect(plain(slots, at::kLong, {k.size(0)}), "slot_map is contiguous int64 [tokens]");
+    const pa_kv4_pool p = kv4_pool(pool, k.size(2));
+    expect(p.n_kv_heads == k.size(1), "the pool has as many heads as k_new and v_new");
+    on_current_device(k, v, pool, slots);
+    run([&] {
+        return pa_kv4_append(&p, k.size(0), k.data_ptr(), v.data_ptr(), {0, k.stride(0), k.stride(1)}, {0, v.stride(0), v.stride(1)},
+                             pool.data_ptr(), (const int64_t *)slots.data_ptr(), stream());
+    });
+    Py_RETURN_NONE;
+}
+
+// kv_pool, slot_map, head_dim, k_out, v_out, dtype
+PyObject *kv4_read(PyObject *const *x)
+{
+    const at::Tensor &pool = tensor(x[0]), &slots = tensor(x[1]);
+    const pa_kv4_pool p = kv4_pool(pool, integer(x[2]));
+    expect(plain(slots, at::kLong, {slots.numel()}), "slot_map is contiguous int64 [tokens]");
+    const int64_t size[3] = {slots.numel(), p.n_kv_heads, p.head_dim};
+    const Out k(x[3], [&] { return make(pool, size, dtype(x[5])); });
+    const Out v(x[4], [&] { return make(pool, size, dtype(x[5])); });
+    expect((is_bf16(k.t) || is_f32(k.t)) && plain(k.t, k.t.scalar_type(), size) && plain(v.t, k.t.scalar_type(), size),
+           "k_out and v_out are contiguous [tokens, head, head_dim], both bfloat16 or both float32");
+    on_current_device(pool, slots, k.t, v.t);
+    run([&] {
+        return pa_kv4_read(&p, slots.numel(), pool.data_ptr(), (const int64_t *)slots.data_ptr(), k.ptr(), v.ptr(),
+                           is_f32(k.t) ? PA_F32 : PA_BF16, stream());
+    });
+    return tuple(k, v);
+}
+
+// q, kv_pool, block_table, cache_lens, window_blocks, sink_blocks, o, lse, workspace, softmax_scale, o_dtype
+PyObject *decode_kv4(PyObject *const *x)
+{
+    const at::Tensor &q = tensor(x[0]), &pool = tensor(x[1]), &table = tensor(x[2]), &lens = tensor(x[3]);
+    expect(q.dim() == 3 && plain(q, at::kBFloat16, q.sizes()), "q is contiguous bfloat16 [batch, head, head_dim]");
+    const Out o(x[6], [&] { return make(q, q.sizes(), dtype(x[10])); });
+    const Out lse(x[7], [&] { return make(q, {q.size(0), q.size(1)}, at::kFloat); });
+    expect((is_bf16(o.t) || is_f32(o.t)) && plain(o.t, o.t.scalar_type(), q.sizes()) &&
+               plain(lse.t, at::kFloat, {q.size(0), q.size(1)}),
+           "o is contiguous as q, bfloat16 or float32; lse float32 [batch, head]");
+    expect(table.dim() == 2 && table.size(1) <= INT32_MAX && plain(table, at::kInt, {q.size(0), table.size(1)}) &&
+               plain(lens, at::kInt, {q.size(0)}),
+           "expected a contiguous int32 block table [batch, max_blocks] and cache_lens [batch]");
+    expect(q.size(0) <= INT32_MAX && q.size(1) <= INT32_MAX, "too large a size");
+    const pa_kv4_params p = {(int32_t)q.size(0), (int32_t)q.size(1), integer32(x[4]), integer32(x[5]), (int32_t)table.size(1),
+                             number(x[9]), is_f32(o.t) ? PA_F32 : PA_BF16, kv4_pool(pool, q.size(2))};
+    const Out ws(x[8], [&] { return make_bytes(q, pa_decode_kv4_workspace_bytes(&p)); });
+    on_current_device(q, pool, table, lens, o.t, lse.t, ws.t);
+    run([&] {
+        return pa_decode_kv4(&p, q.data_ptr(), pool.data_ptr(), (const int32_t *)table.data_ptr(), (const int32_t *)lens.data_ptr(),
+                             o.ptr(), (float *)lse.ptr(), ws.ptr(), (size_t)ws.t.nbytes(), stream());
+    });
+    return tuple(o, lse, ws);
+}
+
 // Wraps a function of N positional arguments.
 template <int N, PyObject *(*F)(PyObject *const *)>
 PyObject *call(PyObject *, PyObject *const *args, Py_ssize_t n)
@@ -363,7 +562,10 @@ PyMethodDef methods[] = {
     {"set_error", set_error, METH_O, nullptr}, PA_METHOD(prefill, 12),       PA_METHOD(prefill_varlen, 13),
     PA_METHOD(prefill_backward, 14),           PA_METHOD(decode, 12),        PA_METHOD(decode_static, 10),
     PA_METHOD(decode_paged, 13),               PA_METHOD(kv_append, 7),
-    PA_METHOD(build_layout, 8),                {nullptr, nullptr, 0, nullptr}};
+    PA_METHOD(build_layout, 8),                PA_METHOD(build_block_tables, 14),
+    PA_METHOD(qk_norm_rope, 10),               PA_METHOD(qk_norm_rope_backward, 15),
+    PA_METHOD(kv4_append, 4),                  PA_METHOD(kv4_read, 6),     PA_METHOD(decode_kv4, 11),
+    {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -16,6 +16,12 @@ pa_status fail(pa_status s, const char *fmt, ...);
 void clear_error();
 
 inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+// Arrays of 32-bit numbers.
+template <typename... P>
+inline bool aligned4(const P *...p)
+{
+    return ((... | reinterpret_cast<uintptr_t>(p)) & 3u) == 0;
+}
 
 constexpr int kMaxDevices = 64;
 
@@ -32,6 +38,7 @@ enum DeviceOnce : int {
     ONCE_PREFILL_ATTR = 0,  // (40: order of the units, head_dim, slots, output type)
     ONCE_DECODE_ATTR = ONCE_PREFILL_ATTR + 40,
     ONCE_BACKWARD_ATTR, ONCE_BACKWARD_ATTR_64, ONCE_BACKWARD_TC_ATTR, ONCE_BACKWARD_TC_ATTR_64,
+    ONCE_KV4_ATTR,
     ONCE_COUNT
 };
 std::mutex &device_once_mutex();

@@ -1,0 +1,194 @@
+"""Refusals of the calls around the attention (tables, norms with rotation, 4-bit cache): before anything is launched."""
+import ctypes
+
+import pytest
+import torch
+
+
+@pytest.fixture(scope="module")
+def b():
+    import paper_2503_03588_b200.binding as binding
+
+    return binding
+
+
+BUF = (ctypes.c_int64 * 64)()
+P = (ctypes.addressof(BUF) + 15) // 16 * 16
+NULL = ctypes.c_void_p(0)
+
+
+def _changed(params, **kv):
+    bad = type(params).from_buffer_copy(params)
+    for k, v in kv.items():
+        if k in ("page_stride", "head_stride", "head_dim", "n_kv_heads", "n_pages", "block") and hasattr(bad, "pool"):
+            setattr(bad.pool, k, v)
+        else:
+            setattr(bad, k, v)
+    return ctypes.byref(bad)
+
+
+def test_tables_refusals(b):
+    good = b.pa_table_params(4, 64, 8, 100, 256, 100)
+
+    def status(p, at=None, value=0, ws=P, ws_bytes=10 ** 6):
+        args = [P] * 10
+        if at is not None:
+            args[at] = value
+        return b.pa_status_string(b.lib.pa_build_block_tables(p, *args, ws, ws_bytes, NULL))
+
+    for bad in (dict(batch=0), dict(max_blocks_per_seq=0), dict(n_pages=0), dict(max_tokens=0), dict(free_capacity=-1)):
+        assert status(_changed(good, **bad)) == "PA_ERR_INVALID_ARG", bad
+        assert b.lib.pa_build_block_tables_workspace_bytes(_changed(good, **bad)) == 0
+    assert status(None) == "PA_ERR_INVALID_ARG"
+    assert status(_changed(good, block=128)) == "PA_ERR_SHAPE"
+    assert status(_changed(good, batch=65536)) == "PA_ERR_SHAPE"
+    for at in range(10):
+        assert status(_changed(good), at) == "PA_ERR_INVALID_ARG", at
+    assert status(_changed(good), 6, P + 4) == "PA_ERR_ALIGNMENT"      # slots are 8 bytes each
+    assert status(_changed(good), 4, P + 2) == "PA_ERR_ALIGNMENT"
+    assert status(_changed(good), ws=0) == status(_changed(good), ws_bytes=16) == "PA_ERR_WORKSPACE"
+    assert status(_changed(good), ws=P + 4) == "PA_ERR_ALIGNMENT"
+
+
+def test_rope_refusals(b):
+    s, o = b.pa_strides(0, 512, 128), b.pa_strides(4096, 512, 128)
+    good = b.pa_rope_params(1, 4, 2, 128, 100, 128, 0, 100, 1e-6, b.PA_BF16, s, s, o, o)
+
+    def forward(p, at=None, value=0):
+        args = [P] * 8
+        if at is not None:
+            args[at] = value
+        return b.pa_status_string(b.lib.pa_qk_norm_rope(p, *args, NULL))
+
+    def backward(p, at=None, value=0, dtype=b.PA_F32, ws=P, ws_bytes=10 ** 7):
+        args = [P] * 12
+        if at is not None:
+            args[at] = value
+        return b.pa_status_string(b.lib.pa_qk_norm_rope_backward(p, *args[:8], dtype, *args[8:], ws, ws_bytes, NULL))
+
+    for call in (forward, backward):
+        for bad in (dict(batch=0), dict(n_q_heads=0), dict(n_kv_heads=0), dict(seq_len=0), dict(max_positions=0), dict(eps=-1.0),
+                    dict(eps=float("nan")), dict(eps=float("inf")), dict(w_dtype=7)):
+            assert call(_changed(good, **bad)) == "PA_ERR_INVALID_ARG", bad
+        for bad in (dict(head_dim=96), dict(rotary_dim=132), dict(rotary_dim=-8), dict(rotary_dim=20), dict(n_q_heads=70000),
+                    dict(seq_len=1 << 40), dict(q=b.pa_strides(0, -8, 128))):
+            assert call(_changed(good, **bad)) == "PA_ERR_SHAPE", bad
+        assert call(_changed(good, k=b.pa_strides(0, 516, 128))) == "PA_ERR_ALIGNMENT"
+        assert call(None) == "PA_ERR_INVALID_ARG"
+        for at in range(8):
+            assert call(_changed(good), at) == "PA_ERR_INVALID_ARG", at
+        for at in (0, 1, 2, 3, 4, 6, 7):
+            assert call(_changed(good), at, P + 8) == "PA_ERR_ALIGNMENT", at
+        assert call(_changed(good), 5, P + 2) == "PA_ERR_ALIGNMENT"
+    for bad in (b.pa_strides(0, 512, 0), b.pa_strides(0, 64, 128)):     # rows written over one another
+        assert forward(_changed(good, q_out=bad)) == "PA_ERR_SHAPE"
+    assert forward(_changed(good, batch=2, k_out=b.pa_strides(0, 512, 128))) == "PA_ERR_SHAPE"
+    assert backward(_changed(good), dtype=9) == "PA_ERR_INVALID_ARG"
+    for at in range(8, 12):
+        assert backward(_changed(good), at) == "PA_ERR_INVALID_ARG", at
+    assert backward(_changed(good), 10, P + 2) == "PA_ERR_ALIGNMENT"
+    assert backward(_changed(good), ws=0) == backward(_changed(good), ws_bytes=100) == "PA_ERR_WORKSPACE"
+    assert backward(_changed(good), ws=P + 4) == "PA_ERR_ALIGNMENT"
+    assert b.lib.pa_qk_norm_rope_backward_workspace_bytes(_changed(good)) == 13 * 2 * 128 * 4   # CTAs of eight tokens
+
+
+def test_kv4_refusals(b):
+    assert b.pa_kv4_page_bytes(128) == 9216 and b.pa_kv4_page_bytes(64) == 4608 and b.pa_kv4_page_bytes(96) == 0
+    good = b.pa_kv4_pool(4, 128, 64, 10, 4 * 9216, 9216)
+    s = b.pa_strides(0, 512, 128)
+
+    def append(p, n=5, k=P, v=P, ks=s, pool=P, slots=P):
+        return b.pa_status_string(b.lib.pa_kv4_append(p, n, k, v, ks, s, pool, slots, NULL))
+
+    def read(p, n=5, pool=P, slots=P, k=P, v=P, dtype=b.PA_F32):
+        return b.pa_status_string(b.lib.pa_kv4_read(p, n, pool, slots, k, v, dtype, NULL))
+
+    for call in (append, read):
+        for bad in (dict(n_kv_heads=0), dict(n_pages=0)):
+            assert call(_changed(good, **bad)) == "PA_ERR_INVALID_ARG", bad
+        for bad in (dict(head_dim=96), dict(block=32), dict(n_kv_heads=70000), dict(head_stride=9200), dict(page_stride=0)):
+            assert call(_changed(good, **bad)) == "PA_ERR_SHAPE", bad
+        assert call(_changed(good, head_stride=9224)) == "PA_ERR_ALIGNMENT"
+        assert call(None) == call(_changed(good), n=-1) == "PA_ERR_INVALID_ARG"
+        assert call(_changed(good), n=0) == "PA_OK"                      # nothing to do, nothing launched
+        assert call(_changed(good), n=1 << 50) == "PA_ERR_SHAPE"
+        for name in ("k", "v", "pool"):
+            assert call(_changed(good), **{name: 0}) == "PA_ERR_INVALID_ARG"
+            assert call(_changed(good), **{name: P + 4}) == "PA_ERR_ALIGNMENT"
+        assert call(_changed(good), slots=0) == "PA_ERR_INVALID_ARG"
+        assert call(_changed(good), slots=P + 4) == "PA_ERR_ALIGNMENT"
+    assert append(_changed(good), ks=b.pa_strides(0, 516, 128)) == "PA_ERR_ALIGNMENT"
+    assert append(_changed(good), ks=b.pa_strides(0, -512, 128)) == "PA_ERR_SHAPE"
+    assert read(_changed(good), dtype=3) == "PA_ERR_INVALID_ARG"
+
+
+def test_decode_kv4_refusals(b):
+    good = b.pa_kv4_params(2, 28, 5, 1, 64, 0.0, b.PA_BF16, b.pa_kv4_pool(4, 128, 64, 10, 4 * 9216, 9216))
+
+    def status(p, at=None, value=0, ws=P, ws_bytes=10 ** 7):
+        args = [P] * 6
+        if at is not None:
+            args[at] = value
+        return b.pa_status_string(b.lib.pa_decode_kv4(p, *args, ws, ws_bytes, NULL))
+
+    for bad in (dict(batch=0), dict(n_q_heads=0), dict(max_blocks_per_seq=0), dict(window_blocks=-1), dict(sink_blocks=-1),
+                dict(o_dtype=5), dict(softmax_scale=-1.0), dict(softmax_scale=float("inf")), dict(softmax_scale=float("nan")),
+                dict(n_pages=0), dict(n_kv_heads=0)):
+        assert status(_changed(good, **bad)) == "PA_ERR_INVALID_ARG", bad
+        assert b.lib.pa_decode_kv4_workspace_bytes(_changed(good, **bad)) == 0
+    for bad in (dict(n_q_heads=30), dict(n_q_heads=36), dict(head_dim=80), dict(block=16), dict(max_blocks_per_seq=1 << 25),
+                dict(batch=70000), dict(window_blocks=5000), dict(sink_blocks=5000), dict(head_stride=9000)):
+        assert status(_changed(good, **bad)) == "PA_ERR_SHAPE", bad
+    assert status(_changed(good, page_stride=4 * 9216 + 8)) == "PA_ERR_ALIGNMENT"
+    for at in range(6):
+        assert status(_changed(good), at) == "PA_ERR_INVALID_ARG", at
+    for at in (0, 1, 4):
+        assert status(_changed(good), at, P + 8) == "PA_ERR_ALIGNMENT", at
+    for at in (2, 3, 5):
+        assert status(_changed(good), at, P + 2) == "PA_ERR_ALIGNMENT", at
+    # a status block of 256 bytes, then (o[128], m, l) per query head and part: the longest row has 1 + 5 + 3 blocks
+    want = 256 + 2 * 28 * 9 * 130 * 4
+    assert b.lib.pa_decode_kv4_workspace_bytes(_changed(good)) == want
+    assert status(_changed(good), ws=0) == status(_changed(good), ws_bytes=want - 1) == "PA_ERR_WORKSPACE"
+    assert status(_changed(good), ws=P + 4) == "PA_ERR_ALIGNMENT"
+
+
+def test_tensors_that_do_not_fit_are_refused(b):
+    """From Python: types, shapes, strides, devices (there is nothing on a GPU here)."""
+    bf = lambda *s: torch.zeros(s, dtype=torch.bfloat16)  # noqa: E731
+    i32 = lambda *s: torch.zeros(s, dtype=torch.int32)    # noqa: E731
+    q, k, w, cs, pos = bf(5, 4, 64), bf(5, 2, 64), bf(64), torch.zeros(9, 64), i32(5)
+    pool, slots = torch.zeros((3, 2, 4608), dtype=torch.uint8), torch.zeros(5, dtype=torch.int64)
+    tab = (i32(2), i32(2), i32(7), i32(1), i32(2, 3), 9, 16)
+
+    def swap(args, **kv):
+        args = list(args)
+        for name, value in kv.items():
+            args[int(name[1:])] = value
+        return args
+
+    rope = (q, k, w, w, cs, pos)
+    cases = [(b.pa_qk_norm_rope, a) for a in (rope, swap(rope, _0=q.float()), swap(rope, _1=bf(4, 2, 64)), swap(rope, _1=bf(5, 2, 128)),
+                                              swap(rope, _2=bf(63)), swap(rope, _2=w.float()), swap(rope, _4=cs.double()),
+                                              swap(rope, _4=cs.T), swap(rope, _5=pos.long()), swap(rope, _5=i32(4)),
+                                              swap(rope, _0=bf(5, 4, 128)[..., ::2]), rope + (q.float(),), rope + (None, bf(5, 3, 64)))]
+    cases += [(b.pa_qk_norm_rope_backward, a) for a in (rope + (q, k), rope + (q, k.float()), rope + (q.half(), k.half()),
+                                                        rope + (k, q), rope + (q, k, q.float()))]
+    cases += [(b.pa_kv4_append, a) for a in ((k, k, pool, slots), (k.float(), k, pool, slots), (k, bf(4, 2, 64), pool, slots),
+                                             (k, k, pool[:, :1], slots), (k, k, pool[..., :4600], slots), (k, k, pool.int(), slots),
+                                             (k, k, pool, slots.int()), (k, k, pool, slots[:4]), (q, q, pool, slots))]
+    cases += [(b.pa_kv4_read, a) for a in ((pool, slots, 64), (pool, slots, 128), (pool, slots.int(), 64), (pool, slots, 1 << 33),
+                                           (pool, slots, 64, k.half(), k.half()), (pool, slots, 64, k, k.float()))]
+    dec = (bf(2, 4, 64), pool, i32(2, 3), i32(2), 5, 1)
+    cases += [(b.pa_decode_kv4, a) for a in (dec, swap(dec, _0=torch.zeros(2, 4, 64)), swap(dec, _2=i32(3, 3)), swap(dec, _2=i32(3, 2).T),
+                                             swap(dec, _3=i32(3)), swap(dec, _3=slots[:2]), swap(dec, _0=bf(2, 4, 128)),
+                                             dec + (bf(2, 4, 32),), dec + (bf(2, 4, 64).half(),), dec + (None, i32(2, 4)))]
+    cases += [(b.pa_build_block_tables, a) for a in (tab, swap(tab, _0=i32(3)), swap(tab, _1=slots[:2]), swap(tab, _3=i32(2)),
+                                                     swap(tab, _4=i32(3, 2).T), swap(tab, _6=-1), tab + (i32(2),), tab + (None, i32(16)))]
+    for f, args in cases:
+        with pytest.raises(AssertionError):
+            f(*args)
+    with pytest.raises(OverflowError):
+        b.pa_build_block_tables(*swap(tab, _5=1 << 40))
+    with pytest.raises(TypeError):
+        b.pa_kv4_append(None, k, pool, slots)
