@@ -18,9 +18,9 @@
 // halfwords of two tokens, put side by side by a byte permutation, are the fragments' key pairs.  Shared memory is read without
 // bank conflicts and without ldmatrix.
 //
-// A CTA is four consumer warps and a producer.  A key block (one page and KV head: 72 D contiguous bytes) is one bulk copy into
-// a ring of stages; warp w takes keys 16 w .. 16 w + 15 of every block and all features, with a maximum, sum and output of
-// its own, and the four are merged at the end of the row.
+// Two kernels.  Few rows (sequence and KV head): kv4_cluster_kernel, a thread-block cluster per row, bound by latency.  Many, or
+// long ones: kv4_range_kernel, every warp of the device an equal share of all rows' blocks, bound by instructions and memory.
+// A key block is one page and KV head, 72 D contiguous bytes, copied to shared memory in bulk.
 #include <cuda_fp16.h>
 #include <math.h>
 
@@ -33,46 +33,24 @@
 
 namespace pa {
 
-constexpr int kD4Consumers = 4;
-constexpr int kD4Threads = 32 * (kD4Consumers + 1);
 constexpr int kD4MaxGroup = 8;
-constexpr int kD4MaxStages = 8;
-constexpr int kD4MaxCluster = 8;
 constexpr size_t kD4StatusBytes = 256;
-constexpr int kD4MaxSmem = 227 * 1024;
+constexpr int kD4MaxSmem = 226 * 1024;  // (227 KB less some static shared memory)
 constexpr long long kD4WaitCycles = 2000000000ll;  // ~1 s
 constexpr float kD4Grow = 6.f;  // the maximum moves once it is exceeded by more than this (weights up to 2^6)
-
-enum Kv4Form { KV4_ROWS = 0, KV4_CLUSTER = 1, KV4_PARTS = 2 };
 
 struct Kv4Args {
     const __nv_bfloat16 *q;
     const uint8_t *pool;
     const int32_t *table, *lens;
-    float *partial;  // [rows G][R][D + 2]
+    float *parts;    // (range kernel) [CTAs][2] results of rows that other CTAs have parts of
     int32_t *status;
     void *o;
     float *lse;
     int64_t page_stride, head_stride, max_len;
-    int32_t table_stride, n_pages, batch, Hkv, G, W, S, R, stages, clear_status, o_is_f32;
-    uint32_t items;
+    int32_t table_stride, n_pages, batch, Hkv, G, W, S, R, stages, clear_status;
     float scale_log2;
     long long wait_cycles;
-};
-
-template <int D>
-struct Kv4Smem {
-    static constexpr uint32_t kStage = Kv4Record<D>::kBytes;
-    static constexpr uint32_t kPartRow = (D + 4) * 4;  // (the pad spreads the heads over the banks)
-    static constexpr uint32_t kPart = kD4Consumers * kD4MaxGroup * kPartRow;
-    static constexpr uint32_t kStat = kD4Consumers * kD4MaxGroup * 8 + 16;  // maximum and sum; whether a warp got there
-    static constexpr uint32_t kRecvRow = (D + 4) * 4;                  // o[D], m, l
-    static constexpr uint32_t kRecv = 14 * kRecvRow;  // R senders x ceil(8 / R) heads
-    static constexpr uint32_t kBars = (2 * kD4MaxStages + 2) * 8;
-    static constexpr size_t bytes(int stages, bool cluster)
-    {
-        return 128 + (size_t)stages * kStage + kPart + kStat + (cluster ? kRecv : 0) + kBars;
-    }
 };
 
 __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
@@ -139,406 +117,449 @@ __device__ __forceinline__ void lds_words(uint32_t addr, uint32_t (&w)[kWords])
     else
         asm volatile("ld.shared.u32 %0, [%1];\n" : "=r"(w[0]) : "r"(addr) : "memory");
 }
-// kForm KV4_ROWS: a persistent grid over the rows (sequence and KV head), results written at once.  KV4_CLUSTER: a row's blocks
-// are dealt to the R CTAs of a cluster, which push their results to the CTA that merges a head (CTA h % R) by asynchronous
-// stores.  KV4_PARTS: dealt to R CTAs anywhere, whose results go to the workspace for kv4_merge_kernel.
-template <int D, bool kF32, int kForm>
-__global__ void __launch_bounds__(kD4Threads, 3) kv4_decode_kernel(const Kv4Args a)
-{
-    using SM = Kv4Smem<D>;
+
+// What a thread (g, t) = (lane / 4, lane % 4) reads of a tile of 16 keys.  Row r < 8 of the 16 x 16 fragments is key r ^ (r / 4)
+// of the tile, row r + 8 that plus 8: a permutation under which a warp's reads of K rows and of V rows fall into different
+// banks.
+template <int D>
+struct Kv4Lane {
     using R4 = Kv4Record<D>;
-    constexpr int NG = R4::kGroups, NW = NG / 2;  // groups; words of a token's scales, or of a V chunk
+    int key;                         // rows g and g + 8 of S: this key and that plus 8
+    uint32_t off_k, off_s;           // in K's half: its words, its scales
+    uint32_t off_v0, off_v1;         // in V's half: the chunks of the keys of columns 2t and 2t + 1
+    __device__ __forceinline__ Kv4Lane(int lane)
+    {
+        const int g = lane >> 2, t = lane & 3;
+        key = g ^ (g >> 2);
+        off_k = (uint32_t)(key * R4::kRow + t * 4 * R4::kGroups);
+        off_s = (uint32_t)(R4::kScales + key * R4::kScaleRow);
+        auto chunk = [&](int r) {
+            const int k = r ^ (r >> 2);
+            return (uint32_t)(k * R4::kRow + (g ^ ((k & 2) << 1)) * 2 * R4::kGroups);
+        };
+        off_v0 = chunk(2 * t);
+        off_v1 = chunk(2 * t + 1);
+    }
+};
+
+// A row's queries as the B operand: head g, features 32 j + 8 t + {0, 4}, {1, 5}, {2, 6}, {3, 7}.
+template <int D>
+struct Kv4Query {
+    static constexpr int NG = D / 32;
+    uint32_t f[NG][4];
+    float c0, c1;  // factors of heads 2t and 2t + 1: the power of two, the softmax scale, log2 e
+    static __device__ __forceinline__ void load(const Kv4Args &a, uint32_t row, int lane, uint4 (&raw)[NG])
+    {
+        const int g = lane >> 2, t = lane & 3;
+        const __nv_bfloat16 *q = a.q + ((int64_t)row * a.G + (g < a.G ? g : 0)) * D + 8 * t;
+#pragma unroll
+        for (int j = 0; j < NG; ++j) raw[j] = g < a.G ? *reinterpret_cast<const uint4 *>(q + 32 * j) : make_uint4(0u, 0u, 0u, 0u);
+    }
+    __device__ __forceinline__ void set(const uint4 (&raw)[NG], float scale_log2, int lane)
+    {
+        const int t = lane & 3;
+        uint32_t top = 0;
+#pragma unroll
+        for (int j = 0; j < NG; ++j)
+            for (uint32_t x : {raw[j].x, raw[j].y, raw[j].z, raw[j].w}) top = max(top, max(x & 0x7fffu, (x >> 16) & 0x7fffu));
+        top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+        const uint32_t field = min(max(top >> 7, 1u), 253u);
+        const float down = __uint_as_float((254u - field) << 23), up = __uint_as_float(field << 23) * scale_log2;
+        c0 = __shfl_sync(0xffffffffu, up, 8 * t);
+        c1 = __shfl_sync(0xffffffffu, up, 8 * t + 4);
+#pragma unroll
+        for (int j = 0; j < NG; ++j) {
+            f[j][0] = cvt_f16x2(bf16_lo(raw[j].x) * down, bf16_lo(raw[j].z) * down);
+            f[j][1] = cvt_f16x2(bf16_hi(raw[j].x) * down, bf16_hi(raw[j].z) * down);
+            f[j][2] = cvt_f16x2(bf16_lo(raw[j].y) * down, bf16_lo(raw[j].w) * down);
+            f[j][3] = cvt_f16x2(bf16_hi(raw[j].y) * down, bf16_hi(raw[j].w) * down);
+        }
+    }
+};
+
+// S^T = K Q^T of the tile at `k` (its first key's place in K's half; the scales lie `ks` behind the half's start): rows g and
+// g + 8 of heads 2t, 2t + 1, in the base-2 domain.
+template <int D>
+__device__ __forceinline__ void kv4_logits(uint32_t half, int tile, const Kv4Lane<D> &at, const Kv4Query<D> &q, float (&sx)[4])
+{
+    using R4 = Kv4Record<D>;
+    constexpr int NG = R4::kGroups, NW = NG / 2;
+    const uint32_t k = half + (uint32_t)(tile * 16 * R4::kRow) + at.off_k, ks = half + (uint32_t)(tile * 16 * R4::kScaleRow) + at.off_s;
+    uint32_t ka[NG], kb[NG], sa[NW], sb[NW];
+    lds_words(k, ka);
+    lds_words(k + 8 * R4::kRow, kb);
+    lds_words(ks, sa);
+    lds_words(ks + 8 * R4::kScaleRow, sb);
+#pragma unroll
+    for (int x = 0; x < 4; ++x) sx[x] = 0.f;
+#pragma unroll
+    for (int j = 0; j < NG; ++j) {
+        float d[4] = {0.f, 0.f, 0.f, 0.f};
+        mma_f16(d, nib_lo(ka[j]), nib_lo(kb[j]), nib_hi(ka[j]), nib_hi(kb[j]), q.f[j][0], q.f[j][1]);
+        const uint32_t u = ka[j] >> 8, v = kb[j] >> 8;
+        mma_f16(d, nib_lo(u), nib_lo(v), nib_hi(u), nib_hi(v), q.f[j][2], q.f[j][3]);
+        const float s0 = j & 1 ? bf16_hi(sa[j / 2]) : bf16_lo(sa[j / 2]);
+        const float s1 = j & 1 ? bf16_hi(sb[j / 2]) : bf16_lo(sb[j / 2]);
+        sx[0] = fmaf(s0, d[0], sx[0]);
+        sx[1] = fmaf(s0, d[1], sx[1]);
+        sx[2] = fmaf(s1, d[2], sx[2]);
+        sx[3] = fmaf(s1, d[3], sx[3]);
+    }
+    sx[0] *= q.c0;
+    sx[1] *= q.c1;
+    sx[2] *= q.c0;
+    sx[3] *= q.c1;
+}
+
+// O^T += V^T P^T of the tile in V's half `half`: p are the weights of rows g, g + 8 and heads 2t, 2t + 1; none_a, none_b: the
+// rows' keys do not exist.  Group by group, the weights times the keys' scales are transposed into the B operand.
+// acc[2 j + h]: features 32 j + 4 g + 2 h + {0, 1}, heads 2t, 2t + 1.
+template <int D, bool kF32>
+__device__ __forceinline__ void kv4_values(uint32_t half, int tile, const Kv4Lane<D> &at, const float (&p)[4], bool none_a, bool none_b,
+                                           float (&acc)[D / 16][4])
+{
+    using R4 = Kv4Record<D>;
+    constexpr int NG = R4::kGroups, NW = NG / 2;
+    const uint32_t v = half + (uint32_t)(tile * 16 * R4::kRow), vs = half + (uint32_t)(tile * 16 * R4::kScaleRow) + at.off_s;
+    uint32_t sa[NW], sb[NW], wa[NW], wb[NW], wc[NW], wd[NW];  // V: the keys of columns 2t, 2t + 1, and these plus 8
+    lds_words(vs, sa);
+    lds_words(vs + 8 * R4::kScaleRow, sb);
+    lds_words(v + at.off_v0, wa);
+    lds_words(v + at.off_v1, wb);
+    lds_words(v + at.off_v0 + 8 * R4::kRow, wc);
+    lds_words(v + at.off_v1 + 8 * R4::kRow, wd);
+#pragma unroll
+    for (int j = 0; j < NG; ++j) {
+        float s0 = j & 1 ? bf16_hi(sa[j / 2]) : bf16_lo(sa[j / 2]);
+        float s1 = j & 1 ? bf16_hi(sb[j / 2]) : bf16_lo(sb[j / 2]);
+        if (none_a) s0 = 0.f;  // (whatever the page holds there)
+        if (none_b) s1 = 0.f;
+        const float w0 = p[0] * s0, w1 = p[1] * s0, w2 = p[2] * s1, w3 = p[3] * s1;
+        const uint32_t h0 = ptx::cvt_bf16x2(w0, w1), h1 = ptx::cvt_bf16x2(w2, w3);
+        const uint32_t b0 = transpose8(h0), b1 = transpose8(h1);
+        uint32_t b2 = 0u, b3 = 0u;
+        if (kF32) {  // what the rounding left
+            b2 = transpose8(ptx::cvt_bf16x2(w0 - bf16_lo(h0), w1 - bf16_hi(h0)));
+            b3 = transpose8(ptx::cvt_bf16x2(w2 - bf16_lo(h1), w3 - bf16_hi(h1)));
+        }
+        const uint32_t sel = j & 1 ? 0x7632u : 0x5410u;
+        uint32_t x = __byte_perm(wa[j / 2], wb[j / 2], sel), y = __byte_perm(wc[j / 2], wd[j / 2], sel);
+#pragma unroll
+        for (int h = 0; h < 2; ++h, x >>= 8, y >>= 8) {
+            const uint32_t a0 = nib_bf16(x), a1 = nib_bf16(x >> 4), a2 = nib_bf16(y), a3 = nib_bf16(y >> 4);
+            mma_b16(acc[2 * j + h], a0, a1, a2, a3, b0, b1);
+            if (kF32) mma_b16(acc[2 * j + h], a0, a1, a2, a3, b2, b3);
+        }
+    }
+}
+
+// What a warp knows of a row: of heads 2t and 2t + 1 the maximum, the sum of weights (this thread's keys) and the output.
+template <int D>
+struct Kv4State {
+    float m0, m1, l0, l1;
+    float acc[D / 16][4];
+    __device__ __forceinline__ void clear()
+    {
+        m0 = m1 = -INFINITY;
+        l0 = l1 = 0.f;
+#pragma unroll
+        for (int e = 0; e < D / 16; ++e) acc[e][0] = acc[e][1] = acc[e][2] = acc[e][3] = 0.f;
+    }
+    // New logits have maxima mx0, mx1 (this thread's).  The maximum is moved only where it is exceeded by far.
+    __device__ __forceinline__ void raise(float mx0, float mx1)
+    {
+#pragma unroll
+        for (int o = 4; o < 32; o *= 2) {
+            mx0 = fmaxf(mx0, __shfl_xor_sync(0xffffffffu, mx0, o));
+            mx1 = fmaxf(mx1, __shfl_xor_sync(0xffffffffu, mx1, o));
+        }
+        const bool up0 = mx0 > m0 + kD4Grow, up1 = mx1 > m1 + kD4Grow;
+        if (__any_sync(0xffffffffu, up0 || up1)) {
+            const float al0 = up0 ? ptx::ex2(m0 - mx0) : 1.f, al1 = up1 ? ptx::ex2(m1 - mx1) : 1.f;
+            m0 = up0 ? mx0 : m0;
+            m1 = up1 ? mx1 : m1;
+            l0 *= al0;
+            l1 *= al1;
+#pragma unroll
+            for (int e = 0; e < D / 16; ++e) {
+                acc[e][0] *= al0;
+                acc[e][1] *= al1;
+                acc[e][2] *= al0;
+                acc[e][3] *= al1;
+            }
+        }
+    }
+    // The weights of logits sx, added to the sums.
+    __device__ __forceinline__ void weigh(const float (&sx)[4], bool none_a, bool none_b, float (&p)[4])
+    {
+        p[0] = none_a ? 0.f : ptx::ex2(sx[0] - m0);
+        p[1] = none_a ? 0.f : ptx::ex2(sx[1] - m1);
+        p[2] = none_b ? 0.f : ptx::ex2(sx[2] - m0);
+        p[3] = none_b ? 0.f : ptx::ex2(sx[3] - m1);
+        l0 += p[0] + p[2];
+        l1 += p[1] + p[3];
+    }
+    __device__ __forceinline__ void sum_up()
+    {
+#pragma unroll
+        for (int o = 4; o < 32; o *= 2) {
+            l0 += __shfl_xor_sync(0xffffffffu, l0, o);
+            l1 += __shfl_xor_sync(0xffffffffu, l1, o);
+        }
+    }
+    // Output, maximum and sum of head h (behind sum_up()) to rows of (D + 4) floats and pairs, h = 0 .. 7.
+    __device__ __forceinline__ void store(uint32_t rows, uint32_t stats, int lane) const
+    {
+        const int g = lane >> 2, t = lane & 3;
+#pragma unroll
+        for (int j = 0; j < D / 32; ++j)
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+                ptx::st_shared_v4(rows + (uint32_t)(2 * t + x) * (D + 4) * 4u + 128u * j + 16u * g, __float_as_uint(acc[2 * j][x]),
+                                  __float_as_uint(acc[2 * j][2 + x]), __float_as_uint(acc[2 * j + 1][x]),
+                                  __float_as_uint(acc[2 * j + 1][2 + x]));
+        if (g == 0)
+            ptx::st_shared_v4(stats + 16u * t, __float_as_uint(m0), __float_as_uint(l0), __float_as_uint(m1), __float_as_uint(l1));
+    }
+};
+
+__device__ __forceinline__ void add_part(float4 &o, const float4 &v, float w)
+{
+    o.x = fmaf(v.x, w, o.x);
+    o.y = fmaf(v.y, w, o.y);
+    o.z = fmaf(v.z, w, o.z);
+    o.w = fmaf(v.w, w, o.w);
+}
+template <bool kF32>
+__device__ __forceinline__ void write4(void *o, int64_t at, const float4 &v, float f)
+{
+    if (kF32)
+        *reinterpret_cast<float4 *>(static_cast<float *>(o) + at) = make_float4(v.x * f, v.y * f, v.z * f, v.w * f);
+    else
+        *reinterpret_cast<uint2 *>(static_cast<__nv_bfloat16 *>(o) + at) =
+            make_uint2(ptx::cvt_bf16x2(v.x * f, v.y * f), ptx::cvt_bf16x2(v.z * f, v.w * f));
+}
+__device__ __forceinline__ float natural(float m, float l) { return (m + log2f(l)) * 0.6931471805599453f; }
+
+// ------------------------------------------------------------------------------------------
+// The cluster kernel.  A row's blocks are dealt to the R CTAs of a cluster.  A CTA is eight consumer warps, which work on two
+// blocks at a time, 16 keys each and all features, with maximum, sum and output of their own, and a warp that fetches the
+// blocks into a ring of stages.  The eight results are merged through shared memory and pushed to the CTA that merges a
+// head (CTA h % R) by asynchronous stores that count their bytes on a barrier of that CTA.
+// ------------------------------------------------------------------------------------------
+constexpr int kC4Consumers = 8;
+constexpr int kC4Threads = 32 * (kC4Consumers + 1);
+constexpr int kC4MaxStages = 8;
+constexpr int kC4MaxCluster = 8;
+
+template <int D>
+struct Kv4ClusterSmem {
+    static constexpr uint32_t kStage = Kv4Record<D>::kBytes;
+    static constexpr uint32_t kRow = (D + 4) * 4;  // (the pad spreads the heads over the banks)
+    static constexpr uint32_t kStat = kC4Consumers * kD4MaxGroup * kRow;
+    static constexpr uint32_t kRecv = kStat + kC4Consumers * kD4MaxGroup * 8;
+    static constexpr uint32_t kBars = kRecv + 14 * kRow;  // R senders x ceil(8 / R) heads: at most 14 (R = 7)
+    static constexpr uint32_t kRest = kBars + (2 * kC4MaxStages + 2) * 8;
+    static constexpr size_t bytes(int stages) { return 128 + (size_t)stages * kStage + kRest; }
+};
+
+template <int D, bool kF32>
+__global__ void __launch_bounds__(kC4Threads, 2) kv4_cluster_kernel(const Kv4Args a)
+{
+    using SM = Kv4ClusterSmem<D>;
+    using R4 = Kv4Record<D>;
     extern __shared__ __align__(128) uint8_t smem_raw[];
     const uint32_t smem = (ptx::smem_u32(smem_raw) + 127u) & ~127u;
     const int stages = a.stages;
-    const uint32_t s_part = smem + (uint32_t)stages * SM::kStage, s_stat = s_part + SM::kPart;
-    const uint32_t s_recv = s_stat + SM::kStat, bars = s_recv + (kForm == KV4_CLUSTER ? SM::kRecv : 0);
+    const uint32_t rest = smem + (uint32_t)stages * SM::kStage, bars = rest + SM::kBars;
     volatile int *abort_flag =
-        reinterpret_cast<volatile int *>(smem_raw + (bars - ptx::smem_u32(smem_raw)) + (2 * kD4MaxStages + 1) * 8);
+        reinterpret_cast<volatile int *>(smem_raw + (bars - ptx::smem_u32(smem_raw)) + (2 * kC4MaxStages + 1) * 8);
     auto bar_full = [&](int s) { return bars + (uint32_t)s * 8u; };
-    auto bar_empty = [&](int s) { return bars + (uint32_t)(kD4MaxStages + s) * 8u; };
-    const uint32_t bar_recv = bars + 2 * kD4MaxStages * 8;
+    auto bar_empty = [&](int s) { return bars + (uint32_t)(kC4MaxStages + s) * 8u; };
+    const uint32_t bar_recv = bars + 2 * kC4MaxStages * 8;
     auto wait_bar = [&](uint32_t b_, uint32_t parity, int code) {
         return ptx::mbar_wait_bounded(b_, parity, abort_flag, a.status, code, a.wait_cycles, (int)PA_ERR_TIMEOUT);
     };
 
-    const int R = kForm == KV4_ROWS ? 1 : a.R, G = a.G;
+    const int R = a.R, G = a.G;
     const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
-    const int g = lane >> 2, t = lane & 3;
-    const int my_r = kForm == KV4_CLUSTER ? (int)(blockIdx.x % (uint32_t)R) : 0;
-    const int heads_here = G > my_r ? (G - my_r + R - 1) / R : 0, heads_per_owner = (kD4MaxGroup + R - 1) / R;
+    const uint32_t row = blockIdx.x / (uint32_t)R;  // = b Hkv + hk
+    const int r = (int)(blockIdx.x - row * (uint32_t)R);
+    const uint32_t b = row / (uint32_t)a.Hkv, hk = row - b * (uint32_t)a.Hkv;
+    const int heads_here = G > r ? (G - r + R - 1) / R : 0, heads_per_owner = (kD4MaxGroup + R - 1) / R;
 
     // Started before the kernel ahead is done: nothing of global memory is touched up to pdl_wait().
     pdl_launch_next();
     if (tid == 0) {
         for (int s = 0; s < stages; ++s) {
             ptx::mbar_init(bar_full(s), 1);
-            ptx::mbar_init(bar_empty(s), kD4Consumers);
+            ptx::mbar_init(bar_empty(s), 4);
         }
-        if (kForm == KV4_CLUSTER) ptx::mbar_init(bar_recv, 1);
+        ptx::mbar_init(bar_recv, 1);
         *abort_flag = 0;
         ptx::fence_barrier_init();
         ptx::fence_proxy_async_smem();
-        if (kForm == KV4_CLUSTER) ptx::mbar_expect_tx(bar_recv, (uint32_t)(heads_here * R) * (D + 2) * 4u);
+        ptx::mbar_expect_tx(bar_recv, (uint32_t)(heads_here * R) * (D + 2) * 4u);
     }
     __syncthreads();
-    if (kForm == KV4_CLUSTER) ptx::cluster_arrive();  // (peers may push here from now on)
+    ptx::cluster_arrive();  // (peers may push here from now on)
     pdl_wait();
-    if (a.clear_status && blockIdx.x == 0 && tid == 0) a.status[0] = 0;
+    const int32_t len_raw = a.lens[b];
+    if (a.clear_status && blockIdx.x == 0 && tid == 0) a.status[0] = 0;  // a wait that gives up (much later) sets it
 
-    const uint32_t it0 = blockIdx.x, it_step = gridDim.x;
-    auto item_len = [&](uint32_t it) -> int32_t { return it < a.items ? a.lens[(it / (uint32_t)R) / (uint32_t)a.Hkv] : 0; };
-    struct Item {
-        uint32_t row;     // sequence x KV heads + KV head
-        int32_t r, len;   // chunk; cache length, 0: invalid
-        int32_t mine;     // blocks of the chunk
-        LayoutRow list;
-    };
-    auto make_item = [&](uint32_t it, int32_t len) {
-        Item w;
-        w.row = it / (uint32_t)R;
-        w.r = (int32_t)(it - w.row * (uint32_t)R);
-        w.len = len >= 1 && len <= a.max_len ? len : 0;
-        w.list = layout_row(w.len ? (w.len - 1) / kKv4Page : 0, a.W, a.S);
-        const int32_t n = w.len ? (int32_t)w.list.n : 0;
-        w.mine = n > w.r ? (n - w.r + R - 1) / R : 0;
-        return w;
-    };
-    int32_t len_next = item_len(it0);
+    const int32_t len = len_raw >= 1 && len_raw <= a.max_len ? len_raw : 0;
+    const LayoutRowOf<int32_t> list = layout_row_of<int32_t>(len ? (len - 1) / kKv4Page : 0, a.W, a.S);
+    const int32_t n = len ? list.n : 0, mine = n > r ? (n - r + R - 1) / R : 0;
 
-    if (wid == kD4Consumers) {
+    if (wid == kC4Consumers) {
         // ------------------------------------------------------------------ producer
         bool ok = true;
-        uint32_t ci = 0;  // blocks issued so far
-        for (uint32_t it = it0; it < a.items; it += it_step) {
-            const Item w = make_item(it, len_next);
-            len_next = item_len(it + it_step);
-            const uint32_t b = w.row / (uint32_t)a.Hkv, hk = w.row - b * (uint32_t)a.Hkv;
-            auto issue = [&](uint32_t at, const uint8_t *src) {
-                const int s = (int)(at % (uint32_t)stages);
-                ptx::mbar_expect_tx(bar_full(s), SM::kStage);
-                ptx::bulk_load(smem + (uint32_t)s * SM::kStage, src, SM::kStage, bar_full(s));
-            };
-            for (int base = 0; base < w.mine; base += 32) {
-                // Each lane finds one block: from the diagonal block (the list's last) backwards, every R-th.
-                const uint8_t *src = a.pool;
-                if (base + lane < w.mine) {
-                    const int32_t j = (int32_t)layout_entry(w.list, w.list.n - 1 - (w.r + (int64_t)(base + lane) * R));
-                    int32_t page = a.table[(int64_t)b * a.table_stride + j];
-                    page = page < 0 ? 0 : page >= a.n_pages ? a.n_pages - 1 : page;
-                    src = a.pool + (int64_t)page * a.page_stride + (int64_t)hk * a.head_stride;
-                }
-                const int count = min(32, w.mine - base);
-                int x = 0;
-                if (ci < (uint32_t)stages) {  // stages that nothing has been in yet: all at once
-                    x = min(count, stages - (int)ci);
-                    if (lane < x) issue(ci + lane, src);
-                }
-                for (; x < count; ++x) {
-                    const uint64_t from = __shfl_sync(0xffffffffu, reinterpret_cast<uint64_t>(src), x);
-                    if (lane == 0 && ok) {
-                        const uint32_t at = ci + x;
-                        ok = wait_bar(bar_empty((int)(at % (uint32_t)stages)), (at / (uint32_t)stages - 1) & 1, 1);
-                        if (ok) issue(at, reinterpret_cast<const uint8_t *>(from));
-                    }
-                }
-                __syncwarp();
-                ci += count;
+        auto issue = [&](int s, const uint8_t *src) {
+            ptx::mbar_expect_tx(bar_full(s), SM::kStage);
+            ptx::bulk_load(smem + (uint32_t)s * SM::kStage, src, SM::kStage, bar_full(s));
+        };
+        int s = 0;
+        uint32_t parity = 1;
+        for (int base = 0; base < mine; base += 32) {
+            // Each lane finds one block: from the diagonal block (the list's last) backwards, every R-th.
+            const uint8_t *src = a.pool;
+            if (base + lane < mine) {
+                const int32_t j = layout_entry<int32_t>(list, n - 1 - (r + (base + lane) * R));
+                int32_t page = a.table[(int64_t)b * a.table_stride + j];
+                page = page < 0 ? 0 : page >= a.n_pages ? a.n_pages - 1 : page;
+                src = a.pool + (int64_t)page * a.page_stride + (int64_t)hk * a.head_stride;
             }
+            const int count = min(32, mine - base);
+            int x = 0;
+            if (base == 0) {  // stages that nothing has been in yet: all at once
+                x = min(count, stages);
+                if (lane < x) issue(lane, src);
+            }
+            for (; x < count; ++x) {
+                const uint64_t from = __shfl_sync(0xffffffffu, reinterpret_cast<uint64_t>(src), x);
+                if (s == 0) parity ^= 1;
+                if (lane == 0 && ok) {
+                    ok = wait_bar(bar_empty(s), parity, 1);
+                    if (ok) issue(s, reinterpret_cast<const uint8_t *>(from));
+                }
+                s = s + 1 == stages ? 0 : s + 1;
+            }
+            __syncwarp();
         }
-        if (kForm == KV4_CLUSTER) ptx::cluster_wait();
+        ptx::cluster_wait();
     } else {
         // ------------------------------------------------------------------ consumers
-        // Row r of the 16 x 16 fragments, r < 8, is key r ^ (r / 4) of the warp's (r >= 8: that plus 8): a permutation
-        // under which the threads' reads of K rows and of V rows fall into different banks.
-        const int key_a = 16 * wid + (g ^ (g >> 2));                                      // rows g (and g + 8) of S
-        const int v0 = 16 * wid + ((2 * t) ^ (t >> 1)), v1 = 16 * wid + ((2 * t + 1) ^ (t >> 1));  // columns 2t, 2t + 1
-        const uint32_t off_k = (uint32_t)key_a * R4::kRow + (uint32_t)t * 4u * NG;
-        const uint32_t off_ks = R4::kScales + (uint32_t)key_a * R4::kScaleRow;
-        auto off_v = [&](int key) { return (uint32_t)(R4::kHalf + key * R4::kRow + (g ^ ((key & 2) << 1)) * 2 * NG); };
-        const uint32_t off_v0 = off_v(v0), off_v1 = off_v(v1);
-
-        uint4 raw[NG];
-        auto load_q = [&](uint32_t it) {
-            const bool in = it < a.items && g < G;
-            const __nv_bfloat16 *qb = a.q + ((int64_t)(in ? it / (uint32_t)R : 0) * G + (in ? g : 0)) * D + 8 * t;
-#pragma unroll
-            for (int j = 0; j < NG; ++j)
-                raw[j] = in ? *reinterpret_cast<const uint4 *>(qb + 32 * j) : make_uint4(0u, 0u, 0u, 0u);
-        };
-        load_q(it0);
+        Kv4Query<D> q;
+        {
+            uint4 raw[D / 32];
+            Kv4Query<D>::load(a, row, lane, raw);
+            q.set(raw, a.scale_log2, lane);
+        }
+        const Kv4Lane<D> at(lane);
+        const int tile = wid & 3;
+        Kv4State<D> st;
+        st.clear();
         bool ok = true;
-        uint32_t ci = 0;
-        for (uint32_t it = it0; it < a.items && ok; it += it_step) {
-            const Item w = make_item(it, len_next);
-            len_next = item_len(it + it_step);
-            // ---- Q as the B operand: head g, features 32 j + 8 t + {0, 4}, {1, 5}, {2, 6}, {3, 7}
-            uint32_t qf[NG][4];
-            float c0, c1;  // factors of heads 2t and 2t + 1: the power of two, the softmax scale, log2 e
-            {
-                uint32_t top = 0;
-#pragma unroll
-                for (int j = 0; j < NG; ++j)
-                    for (uint32_t x : {raw[j].x, raw[j].y, raw[j].z, raw[j].w}) top = max(top, max(x & 0x7fffu, (x >> 16) & 0x7fffu));
-                top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-                top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-                const uint32_t field = min(max(top >> 7, 1u), 253u);
-                const float down = __uint_as_float((254u - field) << 23), up = __uint_as_float(field << 23) * a.scale_log2;
-                c0 = __shfl_sync(0xffffffffu, up, 8 * t);
-                c1 = __shfl_sync(0xffffffffu, up, 8 * t + 4);
-#pragma unroll
-                for (int j = 0; j < NG; ++j) {
-                    qf[j][0] = cvt_f16x2(bf16_lo(raw[j].x) * down, bf16_lo(raw[j].z) * down);
-                    qf[j][1] = cvt_f16x2(bf16_hi(raw[j].x) * down, bf16_hi(raw[j].z) * down);
-                    qf[j][2] = cvt_f16x2(bf16_lo(raw[j].y) * down, bf16_lo(raw[j].w) * down);
-                    qf[j][3] = cvt_f16x2(bf16_hi(raw[j].y) * down, bf16_hi(raw[j].w) * down);
-                }
-            }
-            float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;  // of heads 2t, 2t + 1 (the sums: this thread's keys)
-            float acc[2 * NG][4];  // O^T: tile 2 j + h, rows 32 j + 4 g + 2 h + {0, 1}, heads 2t, 2t + 1
-#pragma unroll
-            for (int e = 0; e < 2 * NG; ++e) acc[e][0] = acc[e][1] = acc[e][2] = acc[e][3] = 0.f;
+        int s = wid >> 2;
+        uint32_t parity = 0;
+        while (s >= stages) {  // (one stage: block 1 is its second phase)
+            s -= stages;
+            parity ^= 1;
+        }
 #pragma unroll 1
-            for (int i = 0; i < w.mine && ok; ++i, ++ci) {
-                const int s = (int)(ci % (uint32_t)stages);
-                const int n_keys = w.r == 0 && i == 0 ? (w.len - 1) % kKv4Page + 1 : kKv4Page;  // (the diagonal block is first)
-                ok = wait_bar(bar_full(s), (ci / (uint32_t)stages) & 1, 2);
-                ok = __all_sync(0xffffffffu, ok);
-                if (!ok) break;
-                if (16 * wid < n_keys) {
-                    const uint32_t st = smem + (uint32_t)s * SM::kStage;
-                    uint32_t ka[NG], kb[NG], sa[NW], sb[NW], va[NW], vb[NW];
-                    lds_words(st + off_k, ka);
-                    lds_words(st + off_k + 8 * R4::kRow, kb);
-                    lds_words(st + off_ks, sa);
-                    lds_words(st + off_ks + 8 * R4::kScaleRow, sb);
-                    lds_words(st + R4::kHalf + off_ks, va);
-                    lds_words(st + R4::kHalf + off_ks + 8 * R4::kScaleRow, vb);
-                    // ---- S^T = K Q^T: keys x heads, group by group
-                    float sx[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                    for (int j = 0; j < NG; ++j) {
-                        float d[4] = {0.f, 0.f, 0.f, 0.f};
-                        mma_f16(d, nib_lo(ka[j]), nib_lo(kb[j]), nib_hi(ka[j]), nib_hi(kb[j]), qf[j][0], qf[j][1]);
-                        const uint32_t u = ka[j] >> 8, v = kb[j] >> 8;
-                        mma_f16(d, nib_lo(u), nib_lo(v), nib_hi(u), nib_hi(v), qf[j][2], qf[j][3]);
-                        const float s0 = j & 1 ? bf16_hi(sa[j / 2]) : bf16_lo(sa[j / 2]);
-                        const float s1 = j & 1 ? bf16_hi(sb[j / 2]) : bf16_lo(sb[j / 2]);
-                        sx[0] = fmaf(s0, d[0], sx[0]);
-                        sx[1] = fmaf(s0, d[1], sx[1]);
-                        sx[2] = fmaf(s1, d[2], sx[2]);
-                        sx[3] = fmaf(s1, d[3], sx[3]);
-                    }
-                    uint32_t wa[NW], wb[NW], wc[NW], wd[NW];  // V: keys v0, v1, v0 + 8, v1 + 8
-                    lds_words(st + off_v0, wa);
-                    lds_words(st + off_v1, wb);
-                    lds_words(st + off_v0 + 8 * R4::kRow, wc);
-                    lds_words(st + off_v1 + 8 * R4::kRow, wd);
-                    sx[0] *= c0;
-                    sx[1] *= c1;
-                    sx[2] *= c0;
-                    sx[3] *= c1;
-                    // Keys that do not exist: no weight, whatever the page holds there.
-                    if (n_keys < kKv4Page) {
-                        if (key_a >= n_keys) {
-                            sx[0] = sx[1] = -INFINITY;
-#pragma unroll
-                            for (int y = 0; y < NW; ++y) va[y] = 0u;
-                        }
-                        if (key_a + 8 >= n_keys) {
-                            sx[2] = sx[3] = -INFINITY;
-#pragma unroll
-                            for (int y = 0; y < NW; ++y) vb[y] = 0u;
-                        }
-                    }
-                    float mx0 = fmaxf(sx[0], sx[2]), mx1 = fmaxf(sx[1], sx[3]);
-#pragma unroll
-                    for (int o = 4; o < 32; o *= 2) {
-                        mx0 = fmaxf(mx0, __shfl_xor_sync(0xffffffffu, mx0, o));
-                        mx1 = fmaxf(mx1, __shfl_xor_sync(0xffffffffu, mx1, o));
-                    }
-                    // The maximum is moved only where it is exceeded by far: the weights stay below 2^6.
-                    const bool up0 = mx0 > m0 + kD4Grow, up1 = mx1 > m1 + kD4Grow;
-                    if (__any_sync(0xffffffffu, up0 || up1)) {
-                        const float al0 = up0 ? ptx::ex2(m0 - mx0) : 1.f, al1 = up1 ? ptx::ex2(m1 - mx1) : 1.f;
-                        m0 = up0 ? mx0 : m0;
-                        m1 = up1 ? mx1 : m1;
-                        l0 *= al0;
-                        l1 *= al1;
-#pragma unroll
-                        for (int e = 0; e < 2 * NG; ++e) {
-                            acc[e][0] *= al0;
-                            acc[e][1] *= al1;
-                            acc[e][2] *= al0;
-                            acc[e][3] *= al1;
-                        }
-                    }
-                    const bool none_a = key_a >= n_keys, none_b = key_a + 8 >= n_keys;
-                    const float p0 = none_a ? 0.f : ptx::ex2(sx[0] - m0), p1 = none_a ? 0.f : ptx::ex2(sx[1] - m1);
-                    const float p2 = none_b ? 0.f : ptx::ex2(sx[2] - m0), p3 = none_b ? 0.f : ptx::ex2(sx[3] - m1);
-                    l0 += p0 + p2;
-                    l1 += p1 + p3;
-                    // ---- O^T += V^T P^T, group by group: the weights times the keys' scales, transposed into the B operand
-#pragma unroll
-                    for (int j = 0; j < NG; ++j) {
-                        const float s0 = j & 1 ? bf16_hi(va[j / 2]) : bf16_lo(va[j / 2]);
-                        const float s1 = j & 1 ? bf16_hi(vb[j / 2]) : bf16_lo(vb[j / 2]);
-                        const float w0 = p0 * s0, w1 = p1 * s0, w2 = p2 * s1, w3 = p3 * s1;
-                        const uint32_t h0 = ptx::cvt_bf16x2(w0, w1), h1 = ptx::cvt_bf16x2(w2, w3);
-                        const uint32_t b0 = transpose8(h0), b1 = transpose8(h1);
-                        uint32_t b2 = 0u, b3 = 0u;
-                        if (kF32) {  // what the rounding left
-                            b2 = transpose8(ptx::cvt_bf16x2(w0 - bf16_lo(h0), w1 - bf16_hi(h0)));
-                            b3 = transpose8(ptx::cvt_bf16x2(w2 - bf16_lo(h1), w3 - bf16_hi(h1)));
-                        }
-                        const uint32_t sel = j & 1 ? 0x7632u : 0x5410u;
-                        uint32_t x = __byte_perm(wa[j / 2], wb[j / 2], sel), y = __byte_perm(wc[j / 2], wd[j / 2], sel);
-#pragma unroll
-                        for (int h = 0; h < 2; ++h, x >>= 8, y >>= 8) {
-                            const uint32_t a0 = nib_bf16(x), a1 = nib_bf16(x >> 4), a2 = nib_bf16(y), a3 = nib_bf16(y >> 4);
-                            mma_b16(acc[2 * j + h], a0, a1, a2, a3, b0, b1);
-                            if (kF32) mma_b16(acc[2 * j + h], a0, a1, a2, a3, b2, b3);
-                        }
-                    }
-                }
-                __syncwarp();
-                if (lane == 0) ptx::mbar_arrive(bar_empty(s));
+        for (int i = wid >> 2; i < mine && ok; i += 2) {
+            const int n_keys = r == 0 && i == 0 ? (len - 1) % kKv4Page + 1 : kKv4Page;  // (the diagonal block is first)
+            ok = wait_bar(bar_full(s), parity, 2);
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) break;
+            if (16 * tile < n_keys) {
+                const uint32_t k_half = smem + (uint32_t)s * SM::kStage;
+                float sx[4], p[4];
+                kv4_logits<D>(k_half, tile, at, q, sx);
+                const bool none_a = 16 * tile + at.key >= n_keys, none_b = 16 * tile + at.key + 8 >= n_keys;
+                if (none_a) sx[0] = sx[1] = -INFINITY;
+                if (none_b) sx[2] = sx[3] = -INFINITY;
+                st.raise(fmaxf(sx[0], sx[2]), fmaxf(sx[1], sx[3]));
+                st.weigh(sx, none_a, none_b, p);
+                kv4_values<D, kF32>(k_half + R4::kHalf, tile, at, p, none_a, none_b, st.acc);
             }
-            load_q(it + it_step);
-
-            // ---- The four warps' results meet in shared memory.
-#pragma unroll
-            for (int o = 4; o < 32; o *= 2) {
-                l0 += __shfl_xor_sync(0xffffffffu, l0, o);
-                l1 += __shfl_xor_sync(0xffffffffu, l1, o);
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(bar_empty(s));
+            s += 2;
+            while (s >= stages) {
+                s -= stages;
+                parity ^= 1;
             }
-            {
-                const uint32_t row0 = s_part + (uint32_t)(wid * kD4MaxGroup + 2 * t) * SM::kPartRow + 16u * g;
-#pragma unroll
-                for (int j = 0; j < NG; ++j)
-#pragma unroll
-                    for (int x = 0; x < 2; ++x)
-                        ptx::st_shared_v4(row0 + x * SM::kPartRow + 128u * j, __float_as_uint(acc[2 * j][x]), __float_as_uint(acc[2 * j][2 + x]),
-                                          __float_as_uint(acc[2 * j + 1][x]), __float_as_uint(acc[2 * j + 1][2 + x]));
-                if (lane == 0) ptx::st_shared(s_stat + kD4Consumers * kD4MaxGroup * 8u + 4u * wid, ok ? 1u : 0u);
-                if (g == 0) {
-                    const uint32_t at = s_stat + (uint32_t)(wid * kD4MaxGroup + 2 * t) * 8u;
-                    ptx::st_shared_v4(at, __float_as_uint(m0), __float_as_uint(l0), __float_as_uint(m1), __float_as_uint(l1));
-                }
-            }
-            asm volatile("bar.sync 1, %0;\n" ::"n"(32 * kD4Consumers) : "memory");
-            // (A wait that gave up ends the loop for all four, or those that go on would wait for the others for good.)
-#pragma unroll
-            for (int x = 0; x < kD4Consumers; ++x)
-                ok = ok && ptx::ld_shared(s_stat + kD4Consumers * kD4MaxGroup * 8u + 4u * x) != 0u;
-            // Thread: head tid / 16, features 4 (tid % 16) + {0 .. 3} (and 64 more).
-            const int h = tid >> 4, f0 = 4 * (tid & 15);
-            float m = -INFINITY, l = 0.f;
-            float4 out[D / 64];
-            {
-                float mw[kD4Consumers], lw[kD4Consumers];
-#pragma unroll
-                for (int x = 0; x < kD4Consumers; ++x) {
-                    ptx::ld_shared_v2(s_stat + (uint32_t)(x * kD4MaxGroup + h) * 8u, mw[x], lw[x]);
-                    m = fmaxf(m, mw[x]);
-                }
-#pragma unroll
-                for (int y = 0; y < D / 64; ++y) out[y] = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-                for (int x = 0; x < kD4Consumers; ++x) {
-                    const float wgt = mw[x] != -INFINITY ? ptx::ex2(mw[x] - m) : 0.f;
-                    l = fmaf(lw[x], wgt, l);
-#pragma unroll
-                    for (int y = 0; y < D / 64; ++y) {
-                        float4 v;
-                        ptx::ld_shared_v4(s_part + (uint32_t)(x * kD4MaxGroup + h) * SM::kPartRow + 4u * (f0 + 64 * y), v.x, v.y, v.z, v.w);
-                        out[y].x = fmaf(v.x, wgt, out[y].x);
-                        out[y].y = fmaf(v.y, wgt, out[y].y);
-                        out[y].z = fmaf(v.z, wgt, out[y].z);
-                        out[y].w = fmaf(v.w, wgt, out[y].w);
-                    }
-                }
-            }
-            if (kForm == KV4_CLUSTER) {
-                ptx::cluster_wait();  // every CTA of the row has set its barrier up
-                if (h < G) {
-                    const uint32_t slot = (uint32_t)(h / R), owner = (uint32_t)(h - (int)slot * R);
-                    const uint32_t dst = ptx::map_shared(s_recv, owner) + ((uint32_t)w.r * (uint32_t)heads_per_owner + slot) * SM::kRecvRow;
-                    const uint32_t their_bar = ptx::map_shared(bar_recv, owner);
-#pragma unroll
-                    for (int y = 0; y < D / 64; ++y) ptx::st_async_v4(dst + 4u * (f0 + 64 * y), out[y], their_bar);
-                    if ((tid & 15) == 0) ptx::st_async_v2(dst + 4u * D, m, l, their_bar);
-                }
-            } else if (h < G) {
-                const int64_t head = (int64_t)w.row * G + h;
-                if (kForm == KV4_PARTS) {
-                    float *dst = a.partial + (head * R + w.r) * (D + 2);
-#pragma unroll
-                    for (int y = 0; y < D / 64; ++y) {
-                        *reinterpret_cast<float2 *>(dst + f0 + 64 * y) = make_float2(out[y].x, out[y].y);
-                        *reinterpret_cast<float2 *>(dst + f0 + 64 * y + 2) = make_float2(out[y].z, out[y].w);
-                    }
-                    if ((tid & 15) == 0) *reinterpret_cast<float2 *>(dst + D) = make_float2(m, l);
-                } else {
-                    const float inv = w.mine > 0 ? 1.0f / l : 0.f;
-#pragma unroll
-                    for (int y = 0; y < D / 64; ++y) {
-                        const int64_t at = head * D + f0 + 64 * y;
-                        const float4 v = make_float4(out[y].x * inv, out[y].y * inv, out[y].z * inv, out[y].w * inv);
-                        if (kF32)
-                            *reinterpret_cast<float4 *>(static_cast<float *>(a.o) + at) = v;
-                        else
-                            *reinterpret_cast<uint2 *>(static_cast<__nv_bfloat16 *>(a.o) + at) =
-                                make_uint2(ptx::cvt_bf16x2(v.x, v.y), ptx::cvt_bf16x2(v.z, v.w));
-                    }
-                    if ((tid & 15) == 0) a.lse[head] = w.mine > 0 ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
-                }
-            }
-            // The area is written again only after every warp has read it.
-            if (kForm != KV4_CLUSTER) asm volatile("bar.sync 1, %0;\n" ::"n"(32 * kD4Consumers) : "memory");
         }
 
-        if (kForm == KV4_CLUSTER && heads_here > 0) {
-            // ---- Heads r, r + R, ... of the row: D threads a head.
+        // ---- The eight warps' results meet in shared memory.
+        st.sum_up();
+        st.store(rest + (uint32_t)(wid * kD4MaxGroup) * SM::kRow, rest + SM::kStat + (uint32_t)(wid * kD4MaxGroup) * 8u, lane);
+        asm volatile("bar.sync 1, %0;\n" ::"n"(32 * kC4Consumers) : "memory");
+        // Warp: a head; thread: features 4 lane + {0 .. 3} (64 features: half the threads).
+        const int h = wid;
+        const uint32_t f0 = 16u * lane;
+        float m = -INFINITY, l = 0.f;
+        float4 out = make_float4(0.f, 0.f, 0.f, 0.f);
+        float mw[kC4Consumers], lw[kC4Consumers];
+#pragma unroll
+        for (int x = 0; x < kC4Consumers; ++x) {
+            ptx::ld_shared_v2(rest + SM::kStat + (uint32_t)(x * kD4MaxGroup + h) * 8u, mw[x], lw[x]);
+            m = fmaxf(m, mw[x]);
+        }
+#pragma unroll
+        for (int x = 0; x < kC4Consumers; ++x) {
+            const float w = mw[x] != -INFINITY ? ptx::ex2(mw[x] - m) : 0.f;
+            l = fmaf(lw[x], w, l);
+            if (4 * lane < D) {
+                float4 v;
+                ptx::ld_shared_v4(rest + (uint32_t)(x * kD4MaxGroup + h) * SM::kRow + f0, v.x, v.y, v.z, v.w);
+                add_part(out, v, w);
+            }
+        }
+        ptx::cluster_wait();  // every CTA of the row has set its barrier up
+        if (h < G) {
+            const uint32_t slot = (uint32_t)(h / R), owner = (uint32_t)(h - (int)slot * R);
+            const uint32_t dst = ptx::map_shared(rest + SM::kRecv, owner) + ((uint32_t)r * (uint32_t)heads_per_owner + slot) * SM::kRow;
+            const uint32_t their_bar = ptx::map_shared(bar_recv, owner);
+            if (4 * lane < D) ptx::st_async_v4(dst + f0, out, their_bar);
+            if (lane == 0) ptx::st_async_v2(dst + 4u * D, m, l, their_bar);
+        }
+
+        // ---- Heads r, r + R, ... of the row, a warp each.
+        if (wid < heads_here) {
             if (!ptx::mbar_wait_bounded_cluster(bar_recv, 0, abort_flag, a.status, 3, a.wait_cycles, (int)PA_ERR_TIMEOUT)) {
-                // This CTA's shared memory has to last until every peer's part is in it: a peer is there after a wait for each of
-                // its blocks at most, so this is over before its own limit is.
+                // This CTA's shared memory has to last until every peer's part is in it: a peer is there after a wait for each
+                // of its blocks at most, so this is over before its own limit is.
                 const long long t0 = clock64(), most = 4 * (a.wait_cycles + 2000000ll) * (2 + (int64_t)a.table_stride / R);
                 while (!ptx::mbar_try_wait_cluster(bar_recv, 0) && clock64() - t0 < most) {
                 }
             } else {
-                const uint32_t row = it0 / (uint32_t)R;
-                constexpr int kPer = 32 * kD4Consumers / D;  // heads at a time
-                for (int slot = tid / D; slot < heads_here; slot += kPer) {
-                    const int d = tid % D, hh = my_r + slot * R;
-                    float m = -INFINITY, l = 0.f, o = 0.f;
-                    float mr[kD4MaxCluster], lr[kD4MaxCluster], orr[kD4MaxCluster];
+                const int slot = wid, hh = r + slot * R;
+                float mr[kC4MaxCluster], lr[kC4MaxCluster];
+                m = -INFINITY;
+                l = 0.f;
+                out = make_float4(0.f, 0.f, 0.f, 0.f);
+                auto src = [&](int x) { return rest + SM::kRecv + (uint32_t)((x < R ? x : 0) * heads_per_owner + slot) * SM::kRow; };
 #pragma unroll
-                    for (int x = 0; x < kD4MaxCluster; ++x) {
-                        const uint32_t src = s_recv + (uint32_t)((x < R ? x : 0) * heads_per_owner + slot) * SM::kRecvRow;
-                        ptx::ld_shared_v2(src + 4u * D, mr[x], lr[x]);
-                        orr[x] = __uint_as_float(ptx::ld_shared(src + 4u * d));
-                    }
-#pragma unroll
-                    for (int x = 0; x < kD4MaxCluster; ++x)
-                        if (x < R) m = fmaxf(m, mr[x]);
-#pragma unroll
-                    for (int x = 0; x < kD4MaxCluster; ++x) {
-                        const float wgt = mr[x] != -INFINITY ? ptx::ex2(mr[x] - m) : 0.f;
-                        if (x < R) {
-                            l = fmaf(lr[x], wgt, l);
-                            o = fmaf(orr[x], wgt, o);
-                        }
-                    }
-                    const bool any = l != 0.f;  // (no key: a length outside [1, max_len])
-                    const float res = any ? o / l : 0.f;
-                    const int64_t head = (int64_t)row * G + hh;
-                    if (kF32)
-                        static_cast<float *>(a.o)[head * D + d] = res;
-                    else
-                        static_cast<__nv_bfloat16 *>(a.o)[head * D + d] = __float2bfloat16_rn(res);
-                    if (d == 0) a.lse[head] = any ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
+                for (int x = 0; x < kC4MaxCluster; ++x) {
+                    ptx::ld_shared_v2(src(x) + 4u * D, mr[x], lr[x]);
+                    if (x < R) m = fmaxf(m, mr[x]);
                 }
+#pragma unroll
+                for (int x = 0; x < kC4MaxCluster; ++x) {
+                    const float w = x < R && mr[x] != -INFINITY ? ptx::ex2(mr[x] - m) : 0.f;
+                    if (x < R) l = fmaf(lr[x], w, l);
+                    if (x < R && 4 * lane < D) {
+                        float4 v;
+                        ptx::ld_shared_v4(src(x) + f0, v.x, v.y, v.z, v.w);
+                        add_part(out, v, w);
+                    }
+                }
+                const int64_t head = (int64_t)row * G + hh;
+                if (4 * lane < D) write4<kF32>(a.o, head * D + 4 * lane, out, n > 0 ? 1.0f / l : 0.f);
+                if (lane == 0) a.lse[head] = n > 0 ? natural(m, l) : -INFINITY;  // (n = 0: a length outside [1, max_len])
             }
         }
     }
@@ -553,43 +574,367 @@ __global__ void __launch_bounds__(kD4Threads, 3) kv4_decode_kernel(const Kv4Args
     }
 }
 
-// The parts of a row's chunks, merged: a CTA per sequence and query head, a thread per feature.
+// ------------------------------------------------------------------------------------------
+// The range kernel.  All blocks of all rows, row after row, are cut into equal ranges, one for each CTA and in it one for
+// each warp: no warp waits for another one before its range is done, and all are done at the same time whatever the lengths
+// are.  A warp takes whole blocks, the halves (K, V) of which it copies into a ring of its own, the next ones as soon as
+// one is free.  A row that lies in a warp's range from end to end is written from its registers; of the others it keeps
+// the first in shared memory and the last in its registers, and behind a barrier the CTA's warps merge these.  A row that
+// other CTAs have parts of goes to the workspace, where kv4_join_kernel merges it.
+// The ranges follow from the lengths, which are on the device: each CTA sums all sequences' blocks up (a thread takes
+// batch / 384 of them), and each thread looks one block of the CTA's range up.
+// ------------------------------------------------------------------------------------------
+constexpr int kR4Warps = 12;
+constexpr int kR4Threads = 32 * kR4Warps;
+constexpr int kR4Ctas = 148;         // CTAs, times a number that keeps every range at no more than a block per thread
+
+template <int D>
+struct Kv4RangeSmem {
+    static constexpr int kHalves = D == 128 ? 3 : 6;                   // halves in a warp's ring
+    static constexpr uint32_t kHalf = Kv4Record<D>::kHalf;
+    static constexpr uint32_t kRing = kHalves * kHalf;                  // of a warp
+    static constexpr uint32_t kRow = (D + 4) * 4;
+    static constexpr uint32_t kPiece = kD4MaxGroup * kRow + kD4MaxGroup * 8;  // rows of eight heads, their maxima and sums
+    static_assert(kPiece <= kRing, "the last pieces take the rings' place");
+    static constexpr uint32_t kFirst = kR4Warps * kRing;                // first pieces
+    static constexpr uint32_t kBars = kFirst + kR4Warps * kPiece;
+    static constexpr uint32_t kDesc = (kBars + kR4Warps * kHalves * 8 + 15) & ~15u;
+    static constexpr uint32_t kSums = kDesc + kR4Threads * 16;          // int32 [threads + 1]
+    static constexpr uint32_t kIds = kSums + (kR4Threads + 4) * 4;      // rows of the pieces, int32 [warps][2]; the abort flag
+    static constexpr size_t bytes() { return 128 + kIds + 2 * kR4Warps * 4 + 16; }
+};
+
+// A row's result in the workspace: its number (-1: none; -2: the CTA has no blocks), then eight heads' maxima, sums and outputs.
+template <int D>
+struct Kv4Part {
+    static constexpr int kFloats = 4 + 2 * kD4MaxGroup + kD4MaxGroup * D;
+};
+
 template <int D, bool kF32>
-__global__ void __launch_bounds__(D) kv4_merge_kernel(const Kv4Args a)
+__global__ void __launch_bounds__(kR4Threads, 1) kv4_range_kernel(const Kv4Args a)
 {
-    __shared__ float s_max[D / 32];
-    const int d = threadIdx.x;
-    const int64_t head = blockIdx.x;
+    using SM = Kv4RangeSmem<D>;
+    constexpr int NH = SM::kHalves;
+    extern __shared__ __align__(128) uint8_t smem_raw[];
+    const uint32_t smem = (ptx::smem_u32(smem_raw) + 127u) & ~127u;
+    uint8_t *base = smem_raw + (smem - ptx::smem_u32(smem_raw));
+    int4 *desc = reinterpret_cast<int4 *>(base + SM::kDesc);  // page, row, blocks left in the row, its blocks and the block's keys
+    int32_t *sums = reinterpret_cast<int32_t *>(base + SM::kSums);
+    int32_t *ids = reinterpret_cast<int32_t *>(base + SM::kIds);
+    volatile int *abort_flag = reinterpret_cast<volatile int *>(ids + 2 * kR4Warps);
+    __shared__ int32_t warp_sums[kR4Warps];
+
+    const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
+    const uint32_t ring = smem + (uint32_t)wid * SM::kRing, bars = smem + SM::kBars + (uint32_t)(wid * NH) * 8u;
+    const int G = a.G;
+
+    pdl_launch_next();
+    if (lane == 0) {
+        for (int s = 0; s < NH; ++s) ptx::mbar_init(bars + 8u * s, 1);
+        ids[2 * wid] = ids[2 * wid + 1] = -1;
+        if (wid == 0) *abort_flag = 0;
+        ptx::fence_barrier_init();
+        ptx::fence_proxy_async_smem();
+    }
+    pdl_wait();
+    if (a.clear_status && blockIdx.x == 0 && tid == 0) a.status[0] = 0;
+
+    // ---- The sequences' blocks, summed up.  Thread: sequences tid per .. tid per + per - 1.
+    const int per = (a.batch + kR4Threads - 1) / kR4Threads;
+    auto row_of = [&](int b, int32_t &len) {
+        len = a.lens[b];
+        if (len < 1 || len > a.max_len) len = 0;
+        LayoutRowOf<int32_t> r = layout_row_of<int32_t>(len ? (len - 1) / kKv4Page : 0, a.W, a.S);
+        if (!len) r.n = 0;
+        return r;
+    };
+    int32_t mine = 0;
+    for (int x = 0; x < per; ++x) {
+        const int b = tid * per + x;
+        int32_t len;
+        if (b < a.batch) mine += row_of(b, len).n * a.Hkv;
+    }
+    int32_t upto = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o *= 2) {
+        const int32_t u = __shfl_up_sync(0xffffffffu, upto, o);
+        if (lane >= o) upto += u;
+    }
+    if (lane == 31) warp_sums[wid] = upto;
+    __syncthreads();
+    int32_t before = 0, total = 0;
+#pragma unroll
+    for (int x = 0; x < kR4Warps; ++x) {
+        const int32_t v = warp_sums[x];
+        before += x < wid ? v : 0;
+        total += v;
+    }
+    sums[tid + 1] = before + upto;
+    if (tid == 0) sums[0] = 0;
+    const int32_t lo = (int32_t)((int64_t)total * blockIdx.x / gridDim.x);
+    const int32_t count = (int32_t)((int64_t)total * (blockIdx.x + 1) / gridDim.x) - lo;  // at most kR4Threads (see the launch)
+    __syncthreads();
+
+    // ---- Thread: one block of the range.
+    if (tid < count) {
+        int k = 0, end = kR4Threads;  // the last k with sums[k] <= lo + tid
+        while (end - k > 1) {
+            const int mid = (k + end) >> 1;
+            if (sums[mid] <= lo + tid) k = mid;
+            else end = mid;
+        }
+        int32_t at = lo + tid - sums[k], len;
+        int b = k * per;
+        LayoutRowOf<int32_t> r = row_of(b, len);
+        while (at >= r.n * a.Hkv) {
+            at -= r.n * a.Hkv;
+            r = row_of(++b, len);
+        }
+        const int32_t hk = at / r.n, i = at - hk * r.n;
+        int32_t page = a.table[(int64_t)b * a.table_stride + layout_entry<int32_t>(r, i)];
+        page = page < 0 ? 0 : page >= a.n_pages ? a.n_pages - 1 : page;
+        const int32_t keys = i == r.n - 1 ? (len - 1) % kKv4Page + 1 : kKv4Page;
+        desc[tid] = make_int4(page, b * a.Hkv + hk, r.n - i, r.n | (keys - 1) << 24);
+    }
+    __syncthreads();
+
+    // ---- Warp: blocks first .. last - 1 of the range.
+    const int first = count * wid / kR4Warps, last = count * (wid + 1) / kR4Warps;
+    auto issue = [&](int x, int half, uint32_t slot) {  // (one lane)
+        const int4 d = desc[x];
+        const uint8_t *src = a.pool + (int64_t)d.x * a.page_stride + (int64_t)(d.y % a.Hkv) * a.head_stride + (half ? SM::kHalf : 0);
+        ptx::mbar_expect_tx(bars + 8u * slot, SM::kHalf);
+        ptx::bulk_load(ring + slot * SM::kHalf, src, SM::kHalf, bars + 8u * slot);
+    };
+    const int halves = 2 * (last - first);
+    if (lane < NH && lane < halves) issue(first + (lane >> 1), lane & 1, (uint32_t)lane);
+    __syncwarp();
+
+    const Kv4Lane<D> at(lane);
+    Kv4Query<D> q;
+    uint4 raw[D / 32];
+    Kv4State<D> st;
+    st.clear();
+    if (first < last) Kv4Query<D>::load(a, (uint32_t)desc[first].y, lane, raw);
+    bool ok = true;
+    uint32_t slot = 0, parity = 0;
+    auto next_slot = [&] {
+        if (++slot == (uint32_t)NH) {
+            slot = 0;
+            parity ^= 1;
+        }
+    };
+    // The half in `slot` has been read by all lanes: half number `x` of the range takes its place.
+    auto refill = [&](int x) {
+        __syncwarp();
+        if (lane == 0 && x < halves) issue(first + (x >> 1), x & 1, slot);
+    };
+    auto wait_half = [&](int code) {
+        ok = ptx::mbar_wait_bounded(bars + 8u * slot, parity, abort_flag, a.status, code, a.wait_cycles, (int)PA_ERR_TIMEOUT);
+        ok = __all_sync(0xffffffffu, ok);
+    };
+    bool row_start = true;  // the next block is its row's first one in this range
+    bool whole = false;     // ... and in the row
+#pragma unroll 1
+    for (int x = first; x < last; ++x) {
+        const int4 d = desc[x];
+        const int n_keys = (int)((uint32_t)d.w >> 24) + 1, n = d.w & 0xffffff;
+        if (row_start) {
+            q.set(raw, a.scale_log2, lane);
+            whole = d.z == n;
+            row_start = false;
+            if (x + d.z < last) Kv4Query<D>::load(a, (uint32_t)desc[x + d.z].y, lane, raw);  // the next row's
+        }
+        wait_half(1);
+        if (!ok) break;
+        float sx[4][4];
+        const uint32_t k_half = ring + slot * SM::kHalf;
+#pragma unroll
+        for (int tile = 0; tile < 4; ++tile) {
+            if (16 * tile < n_keys) {
+                kv4_logits<D>(k_half, tile, at, q, sx[tile]);
+                if (n_keys < kKv4Page) {
+                    if (16 * tile + at.key >= n_keys) sx[tile][0] = sx[tile][1] = -INFINITY;
+                    if (16 * tile + at.key + 8 >= n_keys) sx[tile][2] = sx[tile][3] = -INFINITY;
+                }
+            } else {
+                sx[tile][0] = sx[tile][1] = sx[tile][2] = sx[tile][3] = -INFINITY;
+            }
+        }
+        refill(2 * (x - first) + NH);
+        next_slot();
+        float mx0 = -INFINITY, mx1 = -INFINITY;
+#pragma unroll
+        for (int tile = 0; tile < 4; ++tile) {
+            mx0 = fmaxf(mx0, fmaxf(sx[tile][0], sx[tile][2]));
+            mx1 = fmaxf(mx1, fmaxf(sx[tile][1], sx[tile][3]));
+        }
+        st.raise(mx0, mx1);
+        wait_half(2);
+        if (!ok) break;
+        const uint32_t v_half = ring + slot * SM::kHalf;
+#pragma unroll
+        for (int tile = 0; tile < 4; ++tile)
+            if (16 * tile < n_keys) {
+                float p[4];
+                const bool none_a = 16 * tile + at.key >= n_keys, none_b = 16 * tile + at.key + 8 >= n_keys;
+                st.weigh(sx[tile], none_a, none_b, p);
+                kv4_values<D, kF32>(v_half, tile, at, p, none_a, none_b, st.acc);
+            }
+        refill(2 * (x - first) + 1 + NH);
+        next_slot();
+        if (d.z == 1 && x + 1 < last) {  // the row ends, the range goes on
+            st.sum_up();
+            if (whole) {
+                const int g = lane >> 2, t = lane & 3;
+#pragma unroll
+                for (int y = 0; y < 2; ++y) {
+                    const int h = 2 * t + y;
+                    if (h < G) {
+                        const int64_t head = (int64_t)d.y * G + h;
+                        const float m = y ? st.m1 : st.m0, l = y ? st.l1 : st.l0, inv = 1.0f / l;
+#pragma unroll
+                        for (int j = 0; j < D / 32; ++j)
+                            write4<kF32>(a.o, head * D + 32 * j + 4 * g,
+                                         make_float4(st.acc[2 * j][y], st.acc[2 * j][2 + y], st.acc[2 * j + 1][y], st.acc[2 * j + 1][2 + y]), inv);
+                        if (g == 0) a.lse[head] = natural(m, l);
+                    }
+                }
+            } else {  // (only the range's first row can be this)
+                const uint32_t piece = smem + SM::kFirst + (uint32_t)wid * SM::kPiece;
+                st.store(piece, piece + kD4MaxGroup * SM::kRow, lane);
+                if (lane == 0) ids[2 * wid] = d.y;
+            }
+            st.clear();
+            row_start = true;
+        }
+    }
+    // ---- The last row's piece stays in the ring's place (nothing is on its way to it any more, unless a wait gave up).
+    __syncthreads();
+    if (first < last && ok) {
+        st.sum_up();
+        st.store(ring, ring + kD4MaxGroup * SM::kRow, lane);
+        if (lane == 0) ids[2 * wid + 1] = desc[last - 1].y;
+    }
+    __syncthreads();
+    if (*abort_flag) {
+        if (tid == 0) {  // copies that may still be in flight have a bounded time to land
+            const long long t0 = clock64();
+            while (clock64() - t0 < 2000000ll) {
+            }
+        }
+        return;
+    }
+
+    // ---- Pieces of the same row follow one another.  Warp: every twelfth run of them.
+    float *parts = a.parts + (int64_t)blockIdx.x * 2 * Kv4Part<D>::kFloats;
+    const int32_t row_first = count ? desc[0].y : -1, row_last = count ? desc[count - 1].y : -1;
+    const bool open_first = count && desc[0].z != (desc[0].w & 0xffffff), open_last = count && desc[count - 1].z != 1;
+    int run = 0;
+    for (int x = 0; x < 2 * kR4Warps;) {
+        const int32_t row = ids[x];
+        if (row < 0) {
+            ++x;
+            continue;
+        }
+        int end = x + 1;
+        while (end < 2 * kR4Warps && (ids[end] == row || ids[end] < 0)) ++end;
+        if (run++ % kR4Warps == wid) {
+            // A row that began in an earlier CTA is part 0, one that goes on in the next CTA part 1 (part 0 if both).
+            const bool from_before = open_first && row == row_first, goes_on = open_last && row == row_last;
+            float *part = from_before ? parts : goes_on ? parts + Kv4Part<D>::kFloats : nullptr;
+            for (int h = 0; h < G; ++h) {
+                float m = -INFINITY, l = 0.f;
+                float4 out = make_float4(0.f, 0.f, 0.f, 0.f);
+                auto piece = [&](int y) { return y & 1 ? smem + (uint32_t)(y >> 1) * SM::kRing : smem + SM::kFirst + (uint32_t)(y >> 1) * SM::kPiece; };
+                for (int y = x; y < end; ++y) {
+                    if (ids[y] != row) continue;
+                    float mp, lp;
+                    ptx::ld_shared_v2(piece(y) + kD4MaxGroup * SM::kRow + 8u * h, mp, lp);
+                    m = fmaxf(m, mp);
+                }
+                for (int y = x; y < end; ++y) {
+                    if (ids[y] != row) continue;
+                    float mp, lp;
+                    ptx::ld_shared_v2(piece(y) + kD4MaxGroup * SM::kRow + 8u * h, mp, lp);
+                    const float w = mp != -INFINITY ? ptx::ex2(mp - m) : 0.f;
+                    l = fmaf(lp, w, l);
+                    if (4 * lane < D) {
+                        float4 v;
+                        ptx::ld_shared_v4(piece(y) + (uint32_t)h * SM::kRow + 16u * lane, v.x, v.y, v.z, v.w);
+                        add_part(out, v, w);
+                    }
+                }
+                if (part) {
+                    if (4 * lane < D) *reinterpret_cast<float4 *>(part + 4 + 2 * kD4MaxGroup + h * D + 4 * lane) = out;
+                    if (lane == 0) *reinterpret_cast<float2 *>(part + 4 + 2 * h) = make_float2(m, l);
+                } else {
+                    const int64_t head = (int64_t)row * G + h;
+                    if (4 * lane < D) write4<kF32>(a.o, head * D + 4 * lane, out, 1.0f / l);
+                    if (lane == 0) a.lse[head] = natural(m, l);
+                }
+            }
+        }
+        x = end;
+    }
+    if (tid < 2) {
+        const bool there = tid == 0 ? open_first : open_last && !(open_first && row_first == row_last);
+        reinterpret_cast<int32_t *>(parts + tid * Kv4Part<D>::kFloats)[0] = there ? (tid == 0 ? row_first : row_last) : count ? -1 : -2;
+    }
+
+    // ---- Sequences without a key (a length outside [1, max_len]): zeros.
+    for (int b = blockIdx.x; b < a.batch; b += gridDim.x) {
+        int32_t len;
+        if (row_of(b, len).n) continue;
+        const int heads = a.Hkv * G;
+        for (int x = tid; x < heads * D / 4; x += kR4Threads) write4<kF32>(a.o, (int64_t)b * heads * D + 4 * x, make_float4(0.f, 0.f, 0.f, 0.f), 0.f);
+        for (int x = tid; x < heads; x += kR4Threads) a.lse[(int64_t)b * heads + x] = -INFINITY;
+    }
+}
+
+// Rows that more than one CTA of kv4_range_kernel has a part of: the CTA whose last row goes on in the next ones.  A warp a head.
+template <int D, bool kF32>
+__global__ void __launch_bounds__(32 * kD4MaxGroup) kv4_join_kernel(const Kv4Args a)
+{
+    const int lane = threadIdx.x & 31, h = threadIdx.x >> 5;
     pdl_launch_next();
     pdl_wait();
-    const float *src = a.partial + head * a.R * (D + 2);
-    float m = -INFINITY;
-    for (int c = d; c < a.R; c += D) m = fmaxf(m, src[(int64_t)c * (D + 2) + D]);
-    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-    if ((d & 31) == 0) s_max[d >> 5] = m;
-    __syncthreads();
-#pragma unroll
-    for (int x = 0; x < D / 32; ++x) m = fmaxf(m, s_max[x]);
-    float l = 0.f, o = 0.f;
-#pragma unroll 8
-    for (int c = 0; c < a.R; ++c) {
-        const float *p = src + (int64_t)c * (D + 2);
-        const float mc = p[D], wgt = mc != -INFINITY ? ptx::ex2(mc - m) : 0.f;
-        l = fmaf(p[D + 1], wgt, l);
-        o = fmaf(p[d], wgt, o);
+    const float *part = a.parts + ((int64_t)blockIdx.x * 2 + 1) * Kv4Part<D>::kFloats;
+    const int32_t row = *reinterpret_cast<const int32_t *>(part);
+    if (row < 0 || h >= a.G) return;
+    // Its other parts: part 0 of the next CTAs that have blocks.
+    float m = part[4 + 2 * h], l = part[5 + 2 * h];
+    float4 out = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (4 * lane < D) out = *reinterpret_cast<const float4 *>(part + 4 + 2 * kD4MaxGroup + h * D + 4 * lane);
+    for (unsigned c = blockIdx.x + 1; c < gridDim.x; ++c) {
+        const float *next = a.parts + (int64_t)c * 2 * Kv4Part<D>::kFloats;
+        const int32_t id = *reinterpret_cast<const int32_t *>(next);
+        if (id == -2) continue;
+        if (id != row) break;
+        const float2 s = *reinterpret_cast<const float2 *>(next + 4 + 2 * h);
+        const float top = fmaxf(m, s.x);  // (no number: a part whose logits are all NaN, as its sum)
+        const float w0 = m != -INFINITY ? ptx::ex2(m - top) : 0.f, w1 = s.x != -INFINITY ? ptx::ex2(s.x - top) : 0.f;
+        m = top;
+        l = l * w0 + s.y * w1;
+        if (4 * lane < D) {
+            out = make_float4(out.x * w0, out.y * w0, out.z * w0, out.w * w0);
+            add_part(out, *reinterpret_cast<const float4 *>(next + 4 + 2 * kD4MaxGroup + h * D + 4 * lane), w1);
+        }
     }
-    const bool any = l != 0.f;
-    const float res = any ? o / l : 0.f;
-    if (kF32)
-        static_cast<float *>(a.o)[head * D + d] = res;
-    else
-        static_cast<__nv_bfloat16 *>(a.o)[head * D + d] = __float2bfloat16_rn(res);
-    if (d == 0) a.lse[head] = any ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
+    const int64_t head = (int64_t)row * a.G + h;
+    if (4 * lane < D) write4<kF32>(a.o, head * D + 4 * lane, out, 1.0f / l);
+    if (lane == 0) a.lse[head] = natural(m, l);
 }
 
 // ------------------------------------------------------------------------------------------ host
-constexpr int kD4MaxParts = 64;  // chunks per row in the KV4_PARTS form
-
+// Blocks of the longest row, at most.
+static int kv4_most_blocks(const pa_kv4_params *p)
+{
+    const int64_t rows = p->max_blocks_per_seq, w = p->window_blocks > 1 ? p->window_blocks : 1;
+    int64_t n = w + p->sink_blocks;
+    for (int64_t pw = 1; pw < rows; pw *= 2) n += pw >= w;
+    return (int)(n < rows ? n : rows);
+}
 static pa_status check_kv4(const pa_kv4_params *p)
 {
     if (!p) return fail(PA_ERR_INVALID_ARG, "params must be non-null");
@@ -609,43 +954,60 @@ static pa_status check_kv4(const pa_kv4_params *p)
     if (p->batch > 65535 || p->n_q_heads > 65535) return fail(PA_ERR_SHAPE, "batch and head counts must be <= 65535");
     if (p->window_blocks > 4096 || p->sink_blocks > 4096)
         return fail(PA_ERR_SHAPE, "window_blocks and sink_blocks must be <= 4096");
+    if ((int64_t)p->batch * p->pool.n_kv_heads * kv4_most_blocks(p) > INT32_MAX)
+        return fail(PA_ERR_SHAPE, "more than 2^31 blocks in one call");
     return PA_OK;
 }
 
-static int kv4_stages(int head_dim, int most)
+// CTAs of the range kernel: no range is longer than a block per thread, whatever the lengths are.
+static int64_t kv4_range_ctas(const pa_kv4_params *p)
 {
-    const int n = head_dim == 128 ? 6 : 8;
-    return most < n ? most : n;
-}
-static int kv4_most_blocks(const pa_kv4_params *p)
-{
-    const int64_t rows = p->max_blocks_per_seq, w = p->window_blocks > 1 ? p->window_blocks : 1;
-    int64_t n = w + p->sink_blocks;
-    for (int64_t pw = 1; pw < rows; pw *= 2) n += pw >= w;
-    return (int)(n < rows ? n : rows);
-}
-static size_t kv4_smem(int head_dim, int stages, bool cluster)
-{
-    return head_dim == 128 ? Kv4Smem<128>::bytes(stages, cluster) : Kv4Smem<64>::bytes(stages, cluster);
-}
-// Parts per row, at most: two CTAs a row of 148 x 3 places would be too few otherwise.
-static int kv4_parts(int64_t rows, int most)
-{
-    int64_t R = (148 * 3) / rows;
-    if (R > most / 4) R = most / 4;
-    if (R > kD4MaxParts) R = kD4MaxParts;
-    return R < 1 ? 1 : (int)R;
+    const int64_t blocks = (int64_t)p->batch * p->pool.n_kv_heads * kv4_most_blocks(p);
+    const int64_t turns = (blocks + (int64_t)kR4Ctas * kR4Threads - 1) / ((int64_t)kR4Ctas * kR4Threads);
+    return turns * kR4Ctas;
 }
 
 using Kv4Kernel = void (*)(const Kv4Args);
-static Kv4Kernel kv4_kernel(int head_dim, bool f32, int form)
+// 0: cluster, 1: range, 2: join
+static Kv4Kernel kv4_kernel(int head_dim, bool f32, int which)
 {
     static const Kv4Kernel kernels[2][2][3] = {
-        {{kv4_decode_kernel<64, false, 0>, kv4_decode_kernel<64, false, 1>, kv4_decode_kernel<64, false, 2>},
-         {kv4_decode_kernel<64, true, 0>, kv4_decode_kernel<64, true, 1>, kv4_decode_kernel<64, true, 2>}},
-        {{kv4_decode_kernel<128, false, 0>, kv4_decode_kernel<128, false, 1>, kv4_decode_kernel<128, false, 2>},
-         {kv4_decode_kernel<128, true, 0>, kv4_decode_kernel<128, true, 1>, kv4_decode_kernel<128, true, 2>}}};
-    return kernels[head_dim == 128][f32][form];
+        {{kv4_cluster_kernel<64, false>, kv4_range_kernel<64, false>, kv4_join_kernel<64, false>},
+         {kv4_cluster_kernel<64, true>, kv4_range_kernel<64, true>, kv4_join_kernel<64, true>}},
+        {{kv4_cluster_kernel<128, false>, kv4_range_kernel<128, false>, kv4_join_kernel<128, false>},
+         {kv4_cluster_kernel<128, true>, kv4_range_kernel<128, true>, kv4_join_kernel<128, true>}}};
+    return kernels[head_dim == 128][f32][which];
+}
+static size_t kv4_cluster_smem(int head_dim, int stages)
+{
+    return head_dim == 128 ? Kv4ClusterSmem<128>::bytes(stages) : Kv4ClusterSmem<64>::bytes(stages);
+}
+
+// How many clusters of R CTAs the device holds at once.  Asked once per device and kind of launch.
+static pa_status kv4_resident_clusters(int device, int head_dim, bool f32, int stages, int R, int *out)
+{
+    static std::mutex mu;
+    static int known[kMaxDevices][2][2][kC4MaxStages + 1][kC4MaxCluster + 1];  // the number plus one; 0: not asked yet
+    std::lock_guard<std::mutex> lock(mu);
+    int &n = known[device][head_dim == 128][f32][stages][R];
+    if (n == 0) {
+        cudaLaunchAttribute attr;
+        attr.id = cudaLaunchAttributeClusterDimension;
+        attr.val.clusterDim.x = (unsigned)R;
+        attr.val.clusterDim.y = 1;
+        attr.val.clusterDim.z = 1;
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3((unsigned)R, 1, 1);
+        cfg.blockDim = dim3(kC4Threads, 1, 1);
+        cfg.dynamicSmemBytes = kv4_cluster_smem(head_dim, stages);
+        cfg.attrs = &attr;
+        cfg.numAttrs = 1;
+        int found = 0;
+        PA_CUDA_OK(cudaOccupancyMaxActiveClusters(&found, kv4_kernel(head_dim, f32, 0), &cfg));
+        n = found + 1;
+    }
+    *out = n - 1;
+    return PA_OK;
 }
 
 }  // namespace pa
@@ -654,8 +1016,8 @@ extern "C" size_t pa_decode_kv4_workspace_bytes(const pa_kv4_params *p)
 {
     using namespace pa;
     if (check_kv4(p) != PA_OK) return 0;
-    const int most = kv4_most_blocks(p), parts = kD4MaxParts < most ? kD4MaxParts : most;
-    return kD4StatusBytes + (size_t)p->batch * p->n_q_heads * parts * (p->pool.head_dim + 2) * sizeof(float);
+    const size_t part = sizeof(float) * (p->pool.head_dim == 128 ? Kv4Part<128>::kFloats : Kv4Part<64>::kFloats);
+    return kD4StatusBytes + (size_t)kv4_range_ctas(p) * 2 * part;
 }
 
 extern "C" pa_status pa_decode_kv4(const pa_kv4_params *p, const void *q, const void *kv_pool, const int32_t *block_table,
@@ -678,13 +1040,14 @@ extern "C" pa_status pa_decode_kv4(const pa_kv4_params *p, const void *q, const 
     if (pa_status s = current_sm100_device(&dev)) return s;
 
     const int D = p->pool.head_dim;
+    const bool f32 = p->o_dtype == PA_F32;
     Kv4Args a;
     a.q = static_cast<const __nv_bfloat16 *>(q);
     a.pool = static_cast<const uint8_t *>(kv_pool);
     a.table = block_table;
     a.lens = cache_lens;
     a.status = static_cast<int32_t *>(workspace);
-    a.partial = reinterpret_cast<float *>(static_cast<uint8_t *>(workspace) + kD4StatusBytes);
+    a.parts = reinterpret_cast<float *>(static_cast<uint8_t *>(workspace) + kD4StatusBytes);
     a.o = o;
     a.lse = lse;
     a.page_stride = p->pool.page_stride;
@@ -697,7 +1060,6 @@ extern "C" pa_status pa_decode_kv4(const pa_kv4_params *p, const void *q, const 
     a.G = p->n_q_heads / p->pool.n_kv_heads;
     a.W = p->window_blocks;
     a.S = p->sink_blocks;
-    a.o_is_f32 = p->o_dtype == PA_F32;
     const float scale = p->softmax_scale != 0.f ? p->softmax_scale : 1.0f / sqrtf((float)D);
     a.scale_log2 = scale * 1.4426950408889634f;
     const long long wait_cycles = wait_limit_cycles();
@@ -705,56 +1067,62 @@ extern "C" pa_status pa_decode_kv4(const pa_kv4_params *p, const void *q, const 
     a.clear_status = wait_cycles <= 0;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (!a.clear_status) PA_CUDA_OK(cudaMemsetAsync(a.status, 0, sizeof(int32_t), st));
-
-    const EnvSwitches env = env_switches();
-    const bool f32 = p->o_dtype == PA_F32;
-    const int most = kv4_most_blocks(p);
-    const int64_t rows = (int64_t)a.batch * a.Hkv, places = (int64_t)dev.sms * 3;
-    if (rows > 0x3fffffff / kD4MaxParts) return fail(PA_ERR_SHAPE, "too many rows (%lld)", (long long)rows);
-    int form = rows * 2 <= places ? KV4_CLUSTER : KV4_ROWS, R = 1;
-    if (form == KV4_CLUSTER && kv4_parts(rows, most) > kD4MaxCluster) form = KV4_PARTS;
-    if (env.decode_path == 1) form = KV4_PARTS;
-    if (env.decode_path == 2) form = KV4_CLUSTER;
-    if (env.decode_path == 3) form = KV4_ROWS;
-    if (form != KV4_ROWS) {
-        R = form == KV4_PARTS ? kv4_parts(rows, most) : (int)(places / rows < kD4MaxCluster ? places / rows : kD4MaxCluster);
-        if (env.decode_cluster) R = env.decode_cluster;
-        if (R > most) R = most;
-        if (R < 1) R = 1;
-        if (R == 1 && env.decode_path != 2 && env.decode_path != 1) form = KV4_ROWS;
-    }
-    a.R = R;
-    a.items = (uint32_t)(rows * R);
-    a.stages = env.decode_stages ? env.decode_stages : kv4_stages(D, (most + R - 1) / R);
-
     if (pa_status s = device_once(dev.device, ONCE_KV4_ATTR, [] {
             cudaError_t e = cudaSuccess;
-            for (int i = 0; i < 12; ++i)
-                e = first_error(e, cudaFuncSetAttribute(kv4_kernel(i & 1 ? 128 : 64, i & 2, i / 4),
+            for (int i = 0; i < 8; ++i)
+                e = first_error(e, cudaFuncSetAttribute(kv4_kernel(i & 1 ? 128 : 64, i & 2, i >> 2),
                                                         cudaFuncAttributeMaxDynamicSharedMemorySize, kD4MaxSmem));
             return e;
         }))
         return s;
-    const bool cluster = form == KV4_CLUSTER;
-    cudaLaunchAttribute attr[2];
-    attr[0] = pdl_attribute();
-    attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = (unsigned)R;
-    attr[1].val.clusterDim.y = 1;
-    attr[1].val.clusterDim.z = 1;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(cluster || (int64_t)a.items < places ? a.items : places), 1, 1);
-    cfg.blockDim = dim3(kD4Threads, 1, 1);
-    cfg.dynamicSmemBytes = kv4_smem(D, a.stages, cluster);
-    cfg.stream = st;
-    cfg.attrs = attr;
-    cfg.numAttrs = cluster ? 2 : 1;
-    PA_CUDA_OK(cudaLaunchKernelEx(&cfg, kv4_kernel(D, f32, form), a));
-    if (form != KV4_PARTS) return PA_OK;
-    const dim3 heads((unsigned)((int64_t)a.batch * p->n_q_heads));
-    if (D == 128)
-        PA_CUDA_OK(f32 ? launch_pdl(kv4_merge_kernel<128, true>, heads, 128, 0, st, a) : launch_pdl(kv4_merge_kernel<128, false>, heads, 128, 0, st, a));
-    else
-        PA_CUDA_OK(f32 ? launch_pdl(kv4_merge_kernel<64, true>, heads, 64, 0, st, a) : launch_pdl(kv4_merge_kernel<64, false>, heads, 64, 0, st, a));
+
+    const EnvSwitches env = env_switches();
+    const int most = kv4_most_blocks(p);
+    const int64_t rows = (int64_t)a.batch * a.Hkv;
+    // Clusters where a row gets all the CTAs it can use, two blocks each at most.
+    int R = 0;
+    auto stages_of = [&](int r) {
+        // (Each four warps wait for every other block: if stages are used again their number is even, so that a stage is
+        // always the same four warps', which see each of its phases.)
+        const int n = (most + r - 1) / r, room = env.decode_stages ? env.decode_stages : D == 128 ? 6 : 8;
+        return n <= room ? n : room < 2 ? 2 : room & ~1;
+    };
+    if (env.decode_path != 1 && env.decode_path != 3) {
+        const int64_t fit = (int64_t)dev.sms * 2 / rows;
+        R = env.decode_cluster ? env.decode_cluster : fit < kC4MaxCluster ? (int)fit : kC4MaxCluster;
+        if (R > most) R = most;
+        if (env.decode_path == 2 && R < 1) R = 1;
+        if (env.decode_path != 2 && (R < 1 || (R + 1) * 4 < most)) R = 0;
+        for (; R > 1 && !env.decode_cluster; --R) {
+            int found = 0;
+            if (pa_status s = kv4_resident_clusters(dev.device, D, f32, stages_of(R), R, &found)) return s;
+            if (rows <= found) break;
+        }
+    }
+    if (R > 0) {
+        a.R = R;
+        a.stages = stages_of(R);
+        cudaLaunchAttribute attr[2];
+        attr[0] = pdl_attribute();
+        attr[1].id = cudaLaunchAttributeClusterDimension;
+        attr[1].val.clusterDim.x = (unsigned)R;
+        attr[1].val.clusterDim.y = 1;
+        attr[1].val.clusterDim.z = 1;
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3((unsigned)(rows * R), 1, 1);
+        cfg.blockDim = dim3(kC4Threads, 1, 1);
+        cfg.dynamicSmemBytes = kv4_cluster_smem(D, a.stages);
+        cfg.stream = st;
+        cfg.attrs = attr;
+        cfg.numAttrs = 2;
+        PA_CUDA_OK(cudaLaunchKernelEx(&cfg, kv4_kernel(D, f32, 0), a));
+        return PA_OK;
+    }
+    a.R = 1;
+    a.stages = 0;
+    const unsigned ctas = (unsigned)kv4_range_ctas(p);
+    const size_t smem = D == 128 ? Kv4RangeSmem<128>::bytes() : Kv4RangeSmem<64>::bytes();
+    PA_CUDA_OK(launch_pdl(kv4_kernel(D, f32, 1), dim3(ctas), kR4Threads, smem, st, a));
+    PA_CUDA_OK(launch_pdl(kv4_kernel(D, f32, 2), dim3(ctas), 32 * kD4MaxGroup, 0, st, a));
     return PA_OK;
 }

@@ -13,14 +13,17 @@
 
 namespace pa {
 
-struct LayoutRow {
-    int64_t i, w0;            // the query block, first block of its window
+template <typename Int>
+struct LayoutRowOf {
+    Int i, w0;                // the query block, first block of its window
     int32_t sinks, powers;    // lengths of the first two runs
     int32_t kmax;             // exponent of the first power entry
-    int64_t n;                // entries of the row
+    Int n;                    // entries of the row
 };
+using LayoutRow = LayoutRowOf<int64_t>;
 
-__host__ __device__ inline int64_t layout_clamp(int64_t x, int64_t hi) { return x < 0 ? 0 : x < hi ? x : hi; }
+template <typename Int>
+__host__ __device__ inline Int layout_clamp(Int x, Int hi) { return x < 0 ? 0 : x < hi ? x : hi; }
 
 // floor(log2 x), x >= 1
 __host__ __device__ inline int layout_log2(int64_t x)
@@ -31,31 +34,46 @@ __host__ __device__ inline int layout_log2(int64_t x)
     return 63 - __builtin_clzll((unsigned long long)x);
 #endif
 }
+__host__ __device__ inline int layout_log2(int32_t x)
+{
+#ifdef __CUDA_ARCH__
+    return 31 - __clz(x);
+#else
+    return 31 - __builtin_clz((unsigned)x);
+#endif
+}
 
 // i >= 0, W >= 0, S >= 0.  `power` false drops the power-of-two run: the sliding-window pattern (local window
-// plus sink blocks, Section 3.2 / Section 4.1 "Baseline").
-__host__ __device__ inline LayoutRow layout_row(int64_t i, int32_t W, int32_t S, bool power = true)
+// plus sink blocks, Section 3.2 / Section 4.1 "Baseline").  Int int32_t: i, W and S below 2^29.
+template <typename Int>
+__host__ __device__ inline LayoutRowOf<Int> layout_row_of(Int i, int32_t W, int32_t S, bool power = true)
 {
-    const int64_t w = W > 1 ? W : 1;
-    LayoutRow r;
+    const Int w = W > 1 ? W : 1;
+    LayoutRowOf<Int> r;
     r.i = i;
     r.w0 = i - w + 1 > 0 ? i - w + 1 : 0;
-    r.sinks = (int32_t)layout_clamp(i - w + 1, S);
-    const int k0 = w > 1 ? layout_log2(w - 1) + 1 : 0;  // first k with 2^k >= w
-    r.kmax = power && i - S >= 1 ? layout_log2(i - S) : -1;
+    r.sinks = (int32_t)layout_clamp<Int>(i - w + 1, S);
+    const int k0 = w > 1 ? layout_log2((Int)(w - 1)) + 1 : 0;  // first k with 2^k >= w
+    r.kmax = power && i - S >= 1 ? layout_log2((Int)(i - S)) : -1;
     r.powers = r.kmax >= k0 ? r.kmax - k0 + 1 : 0;
     r.n = (i - r.w0 + 1) + r.sinks + r.powers;
     return r;
 }
+__host__ __device__ inline LayoutRow layout_row(int64_t i, int32_t W, int32_t S, bool power = true)
+{
+    return layout_row_of<int64_t>(i, W, S, power);
+}
 
 // The entry at position pos of the row (0 <= pos < n).
-__host__ __device__ inline int64_t layout_entry(const LayoutRow &r, int64_t pos)
+template <typename Int>
+__host__ __device__ inline Int layout_entry(const LayoutRowOf<Int> &r, Int pos)
 {
     if (pos < r.sinks) return pos;
     pos -= r.sinks;
-    if (pos < r.powers) return r.i - ((int64_t)1 << (r.kmax - (int)pos));
+    if (pos < r.powers) return r.i - ((Int)1 << (r.kmax - (int)pos));
     return r.w0 + pos - r.powers;
 }
+__host__ __device__ inline int64_t layout_entry(const LayoutRow &r, int64_t pos) { return layout_entry<int64_t>(r, pos); }
 
 // Entries of rows 0 .. n - 1.
 __host__ __device__ inline int64_t layout_rows_before(int64_t n, int32_t W, int32_t S, bool power = true)

@@ -203,12 +203,11 @@ def test_decode_kv4(pa, oracle, hq, hkv, d, o_dtype):
 
 
 @pytest.mark.parametrize("env", [{}] + [{"PA_DECODE_PATH": "cluster", "PA_DECODE_CLUSTER": str(r)} for r in range(1, 9)] +
-                         [{"PA_DECODE_PATH": "splitk", "PA_DECODE_CLUSTER": str(r)} for r in (1, 3, 8)] +
                          [{"PA_DECODE_PATH": "splitk"}, {"PA_DECODE_PATH": "persist"}] +
-                         [{"PA_DECODE_PATH": p, "PA_DECODE_STAGES": s} for p in ("persist", "cluster", "splitk") for s in ("1", "2", "5")])
+                         [{"PA_DECODE_PATH": "cluster", "PA_DECODE_STAGES": s, "PA_DECODE_CLUSTER": r} for s in ("1", "2", "5") for r in ("1", "4")])
 @pytest.mark.parametrize("hq,hkv,d", [(14, 2, 128), (4, 1, 64)])
 def test_decode_kv4_forms(pa, oracle, pa_env, hq, hkv, d, env):
-    """The three forms of the kernel, several CTAs per row and ring depths; lengths outside the table among the sequences."""
+    """Both kernels, several CTAs per row and ring depths; lengths outside the table among the sequences."""
     pa_env(**env)
     c = _Cache(pa, [9000, 8193, 0, 130, 7, -5], hkv, d, seed=3, k_scale=2.0)
     c.check(oracle, hq, 5, 1)
@@ -223,17 +222,30 @@ def test_decode_kv4_length_beyond_the_table(pa):
     assert (o[0] == 0).all() and (lse[0] == float("-inf")).all() and torch.isfinite(lse[1]).all()
 
 
-def test_decode_kv4_many_rows(pa, oracle):
-    """More rows than places: several rows a CTA, the ring running on across them."""
+def test_decode_kv4_many_rows(pa, oracle, pa_env):
+    """Equal ranges: warps with many rows, rows in several warps and CTAs, ranges beyond a block per thread, few blocks for
+    all CTAs, more sequences than threads, sequences without a key in between."""
     lens = [int(x) for x in np.random.default_rng(4).integers(1, 1500, 150)]
     c = _Cache(pa, lens, 4, 64, seed=5)
     c.check(oracle, 16, 5, 1)
     c = _Cache(pa, lens, 4, 128, seed=6)
     c.check(oracle, 28, 9, 1, torch.float32)
+    pa_env(PA_DECODE_PATH="persist")
+    c = _Cache(pa, lens[:40], 1, 64, seed=14)
+    c.check(oracle, 1, 5, 1)
+    c = _Cache(pa, [300, 0, 64, 1, -1, 129], 1, 128, seed=15)
+    c.check(oracle, 8, 5, 1, torch.float32)
+    c = _Cache(pa, [0, 0], 2, 64, seed=16)
+    c.check(oracle, 8, 5, 1)
+    short = [int(x) for x in np.random.default_rng(5).integers(-20, 200, 1000)]
+    c = _Cache(pa, short, 1, 64, seed=17)
+    c.check(oracle, 3, 5, 1)
+    c = _Cache(pa, [1] * 500 + [6000] + [1] * 300, 2, 64, seed=18)
+    c.check(oracle, 8, 4096, 1, torch.float32)
 
 
 def test_decode_kv4_long_rows_of_few_sequences(pa, oracle):
-    """A window of 4096 blocks over 70000 tokens: rows in up to 64 parts."""
+    """A window of 4096 blocks over 70000 tokens: a row in all CTAs."""
     c = _Cache(pa, [70001], 1, 128, seed=7)
     c.check(oracle, 7, 4096, 0, torch.float32)
     c.check(oracle, 7, 4096, 0)
@@ -306,7 +318,7 @@ def test_decode_kv4_shared_pages_and_bad_entries(pa, oracle):
     assert torch.equal(o[1:], o2[1:])
 
 
-@pytest.mark.parametrize("path,cluster", [("persist", "1"), ("cluster", "1"), ("cluster", "3"), ("cluster", "8"), ("splitk", "4")])
+@pytest.mark.parametrize("path,cluster", [("persist", "1"), ("cluster", "1"), ("cluster", "3"), ("cluster", "8")])
 def test_decode_kv4_a_wait_that_runs_out_ends_the_kernel(pa, pa_env, path, cluster):
     """Under a limit of one cycle a call ends, with PA_ERR_TIMEOUT or the right result; the calls behind it are right."""
     pa_env(PA_DECODE_PATH=path, PA_DECODE_CLUSTER=cluster, PA_DECODE_STAGES="1")
