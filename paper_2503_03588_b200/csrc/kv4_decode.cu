@@ -13,10 +13,12 @@
 // outputs they come in two parts.
 //
 // The nibbles become 16-bit numbers without conversions: in fp16 (w & 0x000f000f) | 0x6400 is 1024 + u in both halves and
-// (w & 0x00f000f0) | 0x6400 is 1024 + 16 u, in bf16 (w & 0x000f000f) | 0x4300 is 128 + u; one instruction takes u - 8 from
-// each, exactly.  K rows are stored so that a thread's 16 bytes hold its share of every group; V rows so that the same
-// halfwords of two tokens, put side by side by a byte permutation, are the fragments' key pairs.  Shared memory is read without
-// bank conflicts and without ldmatrix.
+// (w & 0x00f000f0) | 0x5400 is 64 + u, in bf16 (w & 0x000f000f) | 0x4300 is 128 + u, each one instruction.  What is too much is
+// taken off by an addition (1024 + u), by the sum that the accumulator starts with (64 + u: -72 sum_i q_i over these
+// features), or by a second product with a constant matrix of -136 (128 + u, a tile of keys at a time, so that nothing large
+// is carried along; fp32 outputs: by an addition).  K rows are stored so that a thread's 16 bytes hold its share of every group; V rows
+// so that the same halfwords of two tokens, put side by side by a byte permutation, are the fragments' key pairs.  Shared
+// memory is read without bank conflicts and without ldmatrix.
 //
 // Two kernels.  Few rows (sequence and KV head): kv4_cluster_kernel, a thread-block cluster per row, bound by latency.  Many, or
 // long ones: kv4_range_kernel, every warp of the device an equal share of all rows' blocks, bound by instructions and memory.
@@ -25,6 +27,7 @@
 #include <math.h>
 
 #include <mutex>
+#include <type_traits>
 
 #include "common.cuh"
 #include "kv4.cuh"
@@ -49,29 +52,31 @@ struct Kv4Args {
     float *lse;
     int64_t page_stride, head_stride, max_len;
     int32_t table_stride, n_pages, batch, Hkv, G, W, S, R, stages, clear_status;
+    int32_t whole_rows;  // (range kernel) ranges begin and end with rows
     float scale_log2;
     long long wait_cycles;
 };
 
+// D(16x8, fp32) = A(16x16, row-major) * B(16x8, column-major) + C, one warp.
 __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
 {
-    asm volatile(
-        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};\n"
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};\n"
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// The same with C = c0 in even columns and c1 in odd ones.
+__device__ __forceinline__ void mma_f16_from(float (&d)[4], float c0, float c1, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
+                                             uint32_t b0, uint32_t b1)
+{
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %11, %10, %11};\n"
+                 : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(c0), "f"(c1));
 }
 __device__ __forceinline__ void mma_b16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
 {
-    asm volatile(
-        "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};\n"
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};\n"
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
-__device__ __forceinline__ uint32_t h2_fma(uint32_t a, uint32_t b, uint32_t c)
-{
-    uint32_t d;
-    asm("fma.rn.f16x2 %0, %1, %2, %3;\n" : "=r"(d) : "r"(a), "r"(b), "r"(c));
-    return d;
 }
 __device__ __forceinline__ uint32_t h2_add(uint32_t a, uint32_t b)
 {
@@ -79,17 +84,30 @@ __device__ __forceinline__ uint32_t h2_add(uint32_t a, uint32_t b)
     asm("add.rn.f16x2 %0, %1, %2;\n" : "=r"(d) : "r"(a), "r"(b));
     return d;
 }
-// The lowest nibble of each half of a word, or the one above it, as fp16 u - 8.
-__device__ __forceinline__ uint32_t nib_lo(uint32_t w) { return h2_add((w & 0x000f000fu) | 0x64006400u, 0xe408e408u); }  // - 1032
-__device__ __forceinline__ uint32_t nib_hi(uint32_t w)
+// (a & b) | c in one instruction: left to itself the compiler takes two, each with a constant of its own.
+__device__ __forceinline__ uint32_t and_or(uint32_t a, uint32_t b, uint32_t c)
 {
-    return h2_fma((w & 0x00f000f0u) | 0x64006400u, 0x2c002c00u, 0xd480d480u);  // / 16 - 72
+    uint32_t d;
+    asm("lop3.b32 %0, %1, %2, %3, 0xea;\n" : "=r"(d) : "r"(a), "r"(b), "r"(c));
+    return d;
 }
-// The lowest nibble of each half as bf16 u - 8.
+// The lowest nibble of each half of a word as fp16 u - 8, and the one above it as 64 + u (kOver more than u - 8).
+__device__ __forceinline__ uint32_t nib_lo(uint32_t w) { return h2_add(and_or(w, 0x000f000fu, 0x64006400u), 0xe408e408u); }  // - 1032
+__device__ __forceinline__ uint32_t nib_hi(uint32_t w) { return and_or(w, 0x00f000f0u, 0x54005400u); }
+constexpr float kOver = 72.f;
+// The lowest nibble of each half as bf16 128 + u, or u - 8.
+__device__ __forceinline__ uint32_t nib_over(uint32_t w) { return and_or(w, 0x000f000fu, 0x43004300u); }
+constexpr uint32_t kMinus136 = 0xc308c308u;
 __device__ __forceinline__ uint32_t nib_bf16(uint32_t w)
 {
     uint32_t d;
-    asm("add.rn.bf16x2 %0, %1, %2;\n" : "=r"(d) : "r"((w & 0x000f000fu) | 0x43004300u), "r"(0xc308c308u));  // - 136
+    asm("add.rn.bf16x2 %0, %1, %2;\n" : "=r"(d) : "r"(nib_over(w)), "r"(kMinus136));
+    return d;
+}
+__device__ __forceinline__ uint32_t bf2_mul(uint32_t a, uint32_t b)
+{
+    uint32_t d;
+    asm("mul.rn.bf16x2 %0, %1, %2;\n" : "=r"(d) : "r"(a), "r"(b));
     return d;
 }
 __device__ __forceinline__ uint32_t cvt_f16x2(float lo, float hi)
@@ -126,19 +144,22 @@ struct Kv4Lane {
     using R4 = Kv4Record<D>;
     int key;                         // rows g and g + 8 of S: this key and that plus 8
     uint32_t off_k, off_s;           // in K's half: its words, its scales
-    uint32_t off_v0, off_v1;         // in V's half: the chunks of the keys of columns 2t and 2t + 1
+    int key0, key1;                  // columns 2t and 2t + 1 of P (and these plus 8 of 2t + 8, 2t + 9)
+    uint32_t off_v0, off_v1;         // in V's half: these keys' chunks, their scales
+    uint32_t off_s0, off_s1;
     __device__ __forceinline__ Kv4Lane(int lane)
     {
         const int g = lane >> 2, t = lane & 3;
         key = g ^ (g >> 2);
         off_k = (uint32_t)(key * R4::kRow + t * 4 * R4::kGroups);
         off_s = (uint32_t)(R4::kScales + key * R4::kScaleRow);
-        auto chunk = [&](int r) {
-            const int k = r ^ (r >> 2);
-            return (uint32_t)(k * R4::kRow + (g ^ ((k & 2) << 1)) * 2 * R4::kGroups);
-        };
-        off_v0 = chunk(2 * t);
-        off_v1 = chunk(2 * t + 1);
+        key0 = (2 * t) ^ (t >> 1);
+        key1 = (2 * t + 1) ^ (t >> 1);
+        auto chunk = [&](int k) { return (uint32_t)(k * R4::kRow + (g ^ ((k & 2) << 1)) * 2 * R4::kGroups); };
+        off_v0 = chunk(key0);
+        off_v1 = chunk(key1);
+        off_s0 = (uint32_t)(R4::kScales + key0 * R4::kScaleRow);
+        off_s1 = (uint32_t)(R4::kScales + key1 * R4::kScaleRow);
     }
 };
 
@@ -147,7 +168,8 @@ template <int D>
 struct Kv4Query {
     static constexpr int NG = D / 32;
     uint32_t f[NG][4];
-    float c0, c1;  // factors of heads 2t and 2t + 1: the power of two, the softmax scale, log2 e
+    float o0[NG], o1[NG];  // of heads 2t and 2t + 1: -72 times the sum of the features {1, 5, 3, 7} of all t
+    float c0, c1;          // of the same heads: the power of two, the softmax scale, log2 e
     static __device__ __forceinline__ void load(const Kv4Args &a, uint32_t row, int lane, uint4 (&raw)[NG])
     {
         const int g = lane >> 2, t = lane & 3;
@@ -164,7 +186,7 @@ struct Kv4Query {
             for (uint32_t x : {raw[j].x, raw[j].y, raw[j].z, raw[j].w}) top = max(top, max(x & 0x7fffu, (x >> 16) & 0x7fffu));
         top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
         top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-        const uint32_t field = min(max(top >> 7, 1u), 253u);
+        const uint32_t field = min(max(top >> 7, 27u), 253u);  // (heads below 2^-100 lose bits)
         const float down = __uint_as_float((254u - field) << 23), up = __uint_as_float(field << 23) * scale_log2;
         c0 = __shfl_sync(0xffffffffu, up, 8 * t);
         c1 = __shfl_sync(0xffffffffu, up, 8 * t + 4);
@@ -174,12 +196,19 @@ struct Kv4Query {
             f[j][1] = cvt_f16x2(bf16_hi(raw[j].x) * down, bf16_hi(raw[j].z) * down);
             f[j][2] = cvt_f16x2(bf16_lo(raw[j].y) * down, bf16_lo(raw[j].w) * down);
             f[j][3] = cvt_f16x2(bf16_hi(raw[j].y) * down, bf16_hi(raw[j].w) * down);
+            const float2 x = __half22float2(*reinterpret_cast<const __half2 *>(&f[j][1]));
+            const float2 y = __half22float2(*reinterpret_cast<const __half2 *>(&f[j][3]));
+            float sum = (x.x + x.y) + (y.x + y.y);
+            sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+            sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+            o0[j] = -kOver * __shfl_sync(0xffffffffu, sum, 8 * t);
+            o1[j] = -kOver * __shfl_sync(0xffffffffu, sum, 8 * t + 4);
         }
     }
 };
 
 // S^T = K Q^T of the tile at `k` (its first key's place in K's half; the scales lie `ks` behind the half's start): rows g and
-// g + 8 of heads 2t, 2t + 1, in the base-2 domain.
+// g + 8 of heads 2t, 2t + 1, not yet times c0 and c1.
 template <int D>
 __device__ __forceinline__ void kv4_logits(uint32_t half, int tile, const Kv4Lane<D> &at, const Kv4Query<D> &q, float (&sx)[4])
 {
@@ -195,8 +224,8 @@ __device__ __forceinline__ void kv4_logits(uint32_t half, int tile, const Kv4Lan
     for (int x = 0; x < 4; ++x) sx[x] = 0.f;
 #pragma unroll
     for (int j = 0; j < NG; ++j) {
-        float d[4] = {0.f, 0.f, 0.f, 0.f};
-        mma_f16(d, nib_lo(ka[j]), nib_lo(kb[j]), nib_hi(ka[j]), nib_hi(kb[j]), q.f[j][0], q.f[j][1]);
+        float d[4];
+        mma_f16_from(d, q.o0[j], q.o1[j], nib_lo(ka[j]), nib_lo(kb[j]), nib_hi(ka[j]), nib_hi(kb[j]), q.f[j][0], q.f[j][1]);
         const uint32_t u = ka[j] >> 8, v = kb[j] >> 8;
         mma_f16(d, nib_lo(u), nib_lo(v), nib_hi(u), nib_hi(v), q.f[j][2], q.f[j][3]);
         const float s0 = j & 1 ? bf16_hi(sa[j / 2]) : bf16_lo(sa[j / 2]);
@@ -206,51 +235,83 @@ __device__ __forceinline__ void kv4_logits(uint32_t half, int tile, const Kv4Lan
         sx[2] = fmaf(s1, d[2], sx[2]);
         sx[3] = fmaf(s1, d[3], sx[3]);
     }
-    sx[0] *= q.c0;
-    sx[1] *= q.c1;
-    sx[2] *= q.c0;
-    sx[3] *= q.c1;
 }
 
-// O^T += V^T P^T of the tile in V's half `half`: p are the weights of rows g, g + 8 and heads 2t, 2t + 1; none_a, none_b: the
-// rows' keys do not exist.  Group by group, the weights times the keys' scales are transposed into the B operand.
-// acc[2 j + h]: features 32 j + 4 g + 2 h + {0, 1}, heads 2t, 2t + 1.
+// O^T += V^T P^T of the tile in V's half `half`: p are the weights of rows g, g + 8 and heads 2t, 2t + 1; of a partial block's
+// tile `keys` exist.  acc[2 j + h]: features 32 j + 4 g + 2 h + {0, 1}, heads 2t, 2t + 1.
+// The weights are transposed into the B operand as bf16 and then multiplied by the keys' scales of each group, two at a time:
+// two roundings, but a quarter of the conversions and transposes.  (fp32 outputs: scaled in fp32, group by group, two parts.)
 template <int D, bool kF32>
-__device__ __forceinline__ void kv4_values(uint32_t half, int tile, const Kv4Lane<D> &at, const float (&p)[4], bool none_a, bool none_b,
+__device__ __forceinline__ void kv4_values(uint32_t half, int tile, const Kv4Lane<D> &at, const float (&p)[4], bool partial, int keys,
                                            float (&acc)[D / 16][4])
 {
     using R4 = Kv4Record<D>;
     constexpr int NG = R4::kGroups, NW = NG / 2;
-    const uint32_t v = half + (uint32_t)(tile * 16 * R4::kRow), vs = half + (uint32_t)(tile * 16 * R4::kScaleRow) + at.off_s;
-    uint32_t sa[NW], sb[NW], wa[NW], wb[NW], wc[NW], wd[NW];  // V: the keys of columns 2t, 2t + 1, and these plus 8
-    lds_words(vs, sa);
-    lds_words(vs + 8 * R4::kScaleRow, sb);
+    const uint32_t v = half + (uint32_t)(tile * 16 * R4::kRow), vs = half + (uint32_t)(tile * 16 * R4::kScaleRow);
+    uint32_t wa[NW], wb[NW], wc[NW], wd[NW];  // the keys of columns 2t, 2t + 1, and these plus 8
     lds_words(v + at.off_v0, wa);
     lds_words(v + at.off_v1, wb);
     lds_words(v + at.off_v0 + 8 * R4::kRow, wc);
     lds_words(v + at.off_v1 + 8 * R4::kRow, wd);
+    uint32_t sa[NW], sb[NW], sc[NW], sd[NW];  // their scales; kF32: sa, sb those of rows g and g + 8
+    lds_words(vs + (kF32 ? at.off_s : at.off_s0), sa);
+    lds_words(vs + (kF32 ? at.off_s + 8 * R4::kScaleRow : at.off_s1), sb);
+    if (!kF32) {
+        lds_words(vs + at.off_s0 + 8 * R4::kScaleRow, sc);
+        lds_words(vs + at.off_s1 + 8 * R4::kScaleRow, sd);
+    }
+    if (partial) {  // (whatever the page holds there)
+#pragma unroll
+        for (int y = 0; y < NW; ++y) {
+            if ((kF32 ? at.key : at.key0) >= keys) sa[y] = 0u;
+            if ((kF32 ? at.key + 8 : at.key1) >= keys) sb[y] = 0u;
+            if (!kF32 && at.key0 + 8 >= keys) sc[y] = 0u;
+            if (!kF32 && at.key1 + 8 >= keys) sd[y] = 0u;
+        }
+    }
+    uint32_t t0 = 0u, t1 = 0u;
+    if (!kF32) {
+        t0 = transpose8(ptx::cvt_bf16x2(p[0], p[1]));
+        t1 = transpose8(ptx::cvt_bf16x2(p[2], p[3]));
+    }
 #pragma unroll
     for (int j = 0; j < NG; ++j) {
-        float s0 = j & 1 ? bf16_hi(sa[j / 2]) : bf16_lo(sa[j / 2]);
-        float s1 = j & 1 ? bf16_hi(sb[j / 2]) : bf16_lo(sb[j / 2]);
-        if (none_a) s0 = 0.f;  // (whatever the page holds there)
-        if (none_b) s1 = 0.f;
-        const float w0 = p[0] * s0, w1 = p[1] * s0, w2 = p[2] * s1, w3 = p[3] * s1;
-        const uint32_t h0 = ptx::cvt_bf16x2(w0, w1), h1 = ptx::cvt_bf16x2(w2, w3);
-        const uint32_t b0 = transpose8(h0), b1 = transpose8(h1);
-        uint32_t b2 = 0u, b3 = 0u;
-        if (kF32) {  // what the rounding left
-            b2 = transpose8(ptx::cvt_bf16x2(w0 - bf16_lo(h0), w1 - bf16_hi(h0)));
-            b3 = transpose8(ptx::cvt_bf16x2(w2 - bf16_lo(h1), w3 - bf16_hi(h1)));
-        }
         const uint32_t sel = j & 1 ? 0x7632u : 0x5410u;
+        uint32_t b0, b1, b2 = 0u, b3 = 0u;
+        if (kF32) {
+            const float s0 = j & 1 ? bf16_hi(sa[j / 2]) : bf16_lo(sa[j / 2]);
+            const float s1 = j & 1 ? bf16_hi(sb[j / 2]) : bf16_lo(sb[j / 2]);
+            const float w0 = p[0] * s0, w1 = p[1] * s0, w2 = p[2] * s1, w3 = p[3] * s1;
+            const uint32_t h0 = ptx::cvt_bf16x2(w0, w1), h1 = ptx::cvt_bf16x2(w2, w3);
+            b0 = transpose8(h0);
+            b1 = transpose8(h1);
+            b2 = transpose8(ptx::cvt_bf16x2(w0 - bf16_lo(h0), w1 - bf16_hi(h0)));  // what the rounding left
+            b3 = transpose8(ptx::cvt_bf16x2(w2 - bf16_lo(h1), w3 - bf16_hi(h1)));
+        } else {
+            b0 = bf2_mul(t0, __byte_perm(sa[j / 2], sb[j / 2], sel));
+            b1 = bf2_mul(t1, __byte_perm(sc[j / 2], sd[j / 2], sel));
+        }
         uint32_t x = __byte_perm(wa[j / 2], wb[j / 2], sel), y = __byte_perm(wc[j / 2], wd[j / 2], sel);
 #pragma unroll
         for (int h = 0; h < 2; ++h, x >>= 8, y >>= 8) {
-            const uint32_t a0 = nib_bf16(x), a1 = nib_bf16(x >> 4), a2 = nib_bf16(y), a3 = nib_bf16(y >> 4);
-            mma_b16(acc[2 * j + h], a0, a1, a2, a3, b0, b1);
-            if (kF32) mma_b16(acc[2 * j + h], a0, a1, a2, a3, b2, b3);
+            if (kF32) {
+                const uint32_t a0 = nib_bf16(x), a1 = nib_bf16(x >> 4), a2 = nib_bf16(y), a3 = nib_bf16(y >> 4);
+                mma_b16(acc[2 * j + h], a0, a1, a2, a3, b0, b1);
+                mma_b16(acc[2 * j + h], a0, a1, a2, a3, b2, b3);
+            } else {
+                mma_b16(acc[2 * j + h], nib_over(x), nib_over(x >> 4), nib_over(y), nib_over(y >> 4), b0, b1);
+                mma_b16(acc[2 * j + h], kMinus136, kMinus136, kMinus136, kMinus136, b0, b1);
+            }
         }
+    }
+}
+
+// Of a partial block's tile the keys from `keys` on do not exist.
+__device__ __forceinline__ void kv4_mask(float (&sx)[4], int key, bool partial, int keys)
+{
+    if (partial) {
+        if (key >= keys) sx[0] = sx[1] = -INFINITY;
+        if (key + 8 >= keys) sx[2] = sx[3] = -INFINITY;
     }
 }
 
@@ -267,8 +328,10 @@ struct Kv4State {
         for (int e = 0; e < D / 16; ++e) acc[e][0] = acc[e][1] = acc[e][2] = acc[e][3] = 0.f;
     }
     // New logits have maxima mx0, mx1 (this thread's).  The maximum is moved only where it is exceeded by far.
-    __device__ __forceinline__ void raise(float mx0, float mx1)
+    __device__ __forceinline__ void raise(float mx0, float mx1, const Kv4Query<D> &q)
     {
+        mx0 *= q.c0;
+        mx1 *= q.c1;
 #pragma unroll
         for (int o = 4; o < 32; o *= 2) {
             mx0 = fmaxf(mx0, __shfl_xor_sync(0xffffffffu, mx0, o));
@@ -290,13 +353,17 @@ struct Kv4State {
             }
         }
     }
-    // The weights of logits sx, added to the sums.
-    __device__ __forceinline__ void weigh(const float (&sx)[4], bool none_a, bool none_b, float (&p)[4])
+    // The weights of logits sx, added to the sums; the tile's keys from `keys` on have none.
+    __device__ __forceinline__ void weigh(const float (&sx)[4], const Kv4Query<D> &q, int key, bool partial, int keys, float (&p)[4])
     {
-        p[0] = none_a ? 0.f : ptx::ex2(sx[0] - m0);
-        p[1] = none_a ? 0.f : ptx::ex2(sx[1] - m1);
-        p[2] = none_b ? 0.f : ptx::ex2(sx[2] - m0);
-        p[3] = none_b ? 0.f : ptx::ex2(sx[3] - m1);
+        p[0] = ptx::ex2(fmaf(sx[0], q.c0, -m0));
+        p[1] = ptx::ex2(fmaf(sx[1], q.c1, -m1));
+        p[2] = ptx::ex2(fmaf(sx[2], q.c0, -m0));
+        p[3] = ptx::ex2(fmaf(sx[3], q.c1, -m1));
+        if (partial) {
+            if (key >= keys) p[0] = p[1] = 0.f;
+            if (key + 8 >= keys) p[2] = p[3] = 0.f;
+        }
         l0 += p[0] + p[2];
         l1 += p[1] + p[3];
     }
@@ -473,16 +540,15 @@ __global__ void __launch_bounds__(kC4Threads, 2) kv4_cluster_kernel(const Kv4Arg
             ok = wait_bar(bar_full(s), parity, 2);
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
+            const bool partial = n_keys < kKv4Page;
             if (16 * tile < n_keys) {
                 const uint32_t k_half = smem + (uint32_t)s * SM::kStage;
                 float sx[4], p[4];
                 kv4_logits<D>(k_half, tile, at, q, sx);
-                const bool none_a = 16 * tile + at.key >= n_keys, none_b = 16 * tile + at.key + 8 >= n_keys;
-                if (none_a) sx[0] = sx[1] = -INFINITY;
-                if (none_b) sx[2] = sx[3] = -INFINITY;
-                st.raise(fmaxf(sx[0], sx[2]), fmaxf(sx[1], sx[3]));
-                st.weigh(sx, none_a, none_b, p);
-                kv4_values<D, kF32>(k_half + R4::kHalf, tile, at, p, none_a, none_b, st.acc);
+                kv4_mask(sx, at.key, partial, n_keys - 16 * tile);
+                st.raise(fmaxf(sx[0], sx[2]), fmaxf(sx[1], sx[3]), q);
+                st.weigh(sx, q, at.key, partial, n_keys - 16 * tile, p);
+                kv4_values<D, kF32>(k_half + R4::kHalf, tile, at, p, partial, n_keys - 16 * tile, st.acc);
             }
             __syncwarp();
             if (lane == 0) ptx::mbar_arrive(bar_empty(s));
@@ -581,6 +647,7 @@ __global__ void __launch_bounds__(kC4Threads, 2) kv4_cluster_kernel(const Kv4Arg
 // one is free.  A row that lies in a warp's range from end to end is written from its registers; of the others it keeps
 // the first in shared memory and the last in its registers, and behind a barrier the CTA's warps merge these.  A row that
 // other CTAs have parts of goes to the workspace, where kv4_join_kernel merges it.
+// Where no row is long, ranges are rounded to whole rows instead, and nothing is left for the second kernel.
 // The ranges follow from the lengths, which are on the device: each CTA sums all sequences' blocks up (a thread takes
 // batch / 384 of them), and each thread looks one block of the CTA's range up.
 // ------------------------------------------------------------------------------------------
@@ -590,7 +657,7 @@ constexpr int kR4Ctas = 148;         // CTAs, times a number that keeps every ra
 
 template <int D>
 struct Kv4RangeSmem {
-    static constexpr int kHalves = D == 128 ? 3 : 6;                   // halves in a warp's ring
+    static constexpr int kHalves = D == 128 ? 2 : 4;                   // halves in a warp's ring
     static constexpr uint32_t kHalf = Kv4Record<D>::kHalf;
     static constexpr uint32_t kRing = kHalves * kHalf;                  // of a warp
     static constexpr uint32_t kRow = (D + 4) * 4;
@@ -599,8 +666,8 @@ struct Kv4RangeSmem {
     static constexpr uint32_t kFirst = kR4Warps * kRing;                // first pieces
     static constexpr uint32_t kBars = kFirst + kR4Warps * kPiece;
     static constexpr uint32_t kDesc = (kBars + kR4Warps * kHalves * 8 + 15) & ~15u;
-    static constexpr uint32_t kSums = kDesc + kR4Threads * 16;          // int32 [threads + 1]
-    static constexpr uint32_t kIds = kSums + (kR4Threads + 4) * 4;      // rows of the pieces, int32 [warps][2]; the abort flag
+    static constexpr uint32_t kSums = kDesc + kR4Threads * 16;
+    static constexpr uint32_t kIds = kSums + kR4Threads * 8;      // rows of the pieces, int32 [warps][2]; the abort flag
     static constexpr size_t bytes() { return 128 + kIds + 2 * kR4Warps * 4 + 16; }
 };
 
@@ -618,8 +685,9 @@ __global__ void __launch_bounds__(kR4Threads, 1) kv4_range_kernel(const Kv4Args 
     extern __shared__ __align__(128) uint8_t smem_raw[];
     const uint32_t smem = (ptx::smem_u32(smem_raw) + 127u) & ~127u;
     uint8_t *base = smem_raw + (smem - ptx::smem_u32(smem_raw));
-    int4 *desc = reinterpret_cast<int4 *>(base + SM::kDesc);  // page, row, blocks left in the row, its blocks and the block's keys
-    int32_t *sums = reinterpret_cast<int32_t *>(base + SM::kSums);
+    // A block: where its record is (two words), its row, the blocks left in the row | keys - 1 << 24 | first in the row << 30
+    int4 *desc = reinterpret_cast<int4 *>(base + SM::kDesc);
+    int2 *sums = reinterpret_cast<int2 *>(base + SM::kSums);  // a thread's first block, and the length of its only sequence
     int32_t *ids = reinterpret_cast<int32_t *>(base + SM::kIds);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(ids + 2 * kR4Warps);
     __shared__ int32_t warp_sums[kR4Warps];
@@ -641,18 +709,22 @@ __global__ void __launch_bounds__(kR4Threads, 1) kv4_range_kernel(const Kv4Args 
 
     // ---- The sequences' blocks, summed up.  Thread: sequences tid per .. tid per + per - 1.
     const int per = (a.batch + kR4Threads - 1) / kR4Threads;
-    auto row_of = [&](int b, int32_t &len) {
-        len = a.lens[b];
-        if (len < 1 || len > a.max_len) len = 0;
+    auto row_of = [&](int32_t len) {
         LayoutRowOf<int32_t> r = layout_row_of<int32_t>(len ? (len - 1) / kKv4Page : 0, a.W, a.S);
         if (!len) r.n = 0;
         return r;
     };
-    int32_t mine = 0;
+    auto len_of = [&](int b) {
+        const int32_t len = a.lens[b];
+        return len >= 1 && len <= a.max_len ? len : 0;
+    };
+    int32_t mine = 0, my_len = 0;  // (the length of its only sequence)
     for (int x = 0; x < per; ++x) {
         const int b = tid * per + x;
-        int32_t len;
-        if (b < a.batch) mine += row_of(b, len).n * a.Hkv;
+        if (b < a.batch) {
+            my_len = len_of(b);
+            mine += row_of(my_len).n * a.Hkv;
+        }
     }
     int32_t upto = mine;
 #pragma unroll
@@ -669,53 +741,57 @@ __global__ void __launch_bounds__(kR4Threads, 1) kv4_range_kernel(const Kv4Args 
         before += x < wid ? v : 0;
         total += v;
     }
-    sums[tid + 1] = before + upto;
-    if (tid == 0) sums[0] = 0;
-    const int32_t lo = (int32_t)((int64_t)total * blockIdx.x / gridDim.x);
-    const int32_t count = (int32_t)((int64_t)total * (blockIdx.x + 1) / gridDim.x) - lo;  // at most kR4Threads (see the launch)
+    sums[tid] = make_int2(before + upto - mine, my_len);
+    const int32_t lo = (int32_t)((int64_t)total * blockIdx.x / gridDim.x), hi = (int32_t)((int64_t)total * (blockIdx.x + 1) / gridDim.x);
     __syncthreads();
 
-    // ---- Thread: one block of the range.
-    if (tid < count) {
-        int k = 0, end = kR4Threads;  // the last k with sums[k] <= lo + tid
+    // ---- Thread: block lo + tid.  It belongs to the range if it lies in [lo, hi), or if its row begins there (whole_rows).
+    bool inside = false, earlier = false;
+    int4 found = make_int4(0, 0, 0, 0);
+    if (lo + tid < (a.whole_rows ? total : hi)) {
+        int k = 0, end = kR4Threads;  // the last k whose sequences begin at or before this block
         while (end - k > 1) {
             const int mid = (k + end) >> 1;
-            if (sums[mid] <= lo + tid) k = mid;
+            if (sums[mid].x <= lo + tid) k = mid;
             else end = mid;
         }
-        int32_t at = lo + tid - sums[k], len;
+        int32_t at = lo + tid - sums[k].x, len = per == 1 ? sums[k].y : len_of(k * per);
         int b = k * per;
-        LayoutRowOf<int32_t> r = row_of(b, len);
+        LayoutRowOf<int32_t> r = row_of(len);
         while (at >= r.n * a.Hkv) {
             at -= r.n * a.Hkv;
-            r = row_of(++b, len);
+            len = len_of(++b);
+            r = row_of(len);
         }
-        const int32_t hk = at / r.n, i = at - hk * r.n;
-        int32_t page = a.table[(int64_t)b * a.table_stride + layout_entry<int32_t>(r, i)];
-        page = page < 0 ? 0 : page >= a.n_pages ? a.n_pages - 1 : page;
-        const int32_t keys = i == r.n - 1 ? (len - 1) % kKv4Page + 1 : kKv4Page;
-        desc[tid] = make_int4(page, b * a.Hkv + hk, r.n - i, r.n | (keys - 1) << 24);
+        const int32_t hk = at / r.n, i = at - hk * r.n, begin = lo + tid - i;
+        earlier = a.whole_rows && begin < lo;
+        inside = !a.whole_rows || (begin >= lo && begin < hi);
+        if (inside) {
+            int32_t page = a.table[(int64_t)b * a.table_stride + layout_entry<int32_t>(r, i)];
+            page = page < 0 ? 0 : page >= a.n_pages ? a.n_pages - 1 : page;
+            const int32_t keys = i == r.n - 1 ? (len - 1) % kKv4Page + 1 : kKv4Page;
+            const int64_t src = (int64_t)page * a.page_stride + (int64_t)hk * a.head_stride;
+            found = make_int4((int)(uint32_t)src, (int)(src >> 32), b * a.Hkv + hk, (r.n - i) | (keys - 1) << 24 | (i == 0) << 30);
+        }
     }
-    __syncthreads();
+    const int skipped = a.whole_rows ? __syncthreads_count(earlier) : 0;  // (the first ones)
+    if (inside) desc[tid - skipped] = found;
+    const int count = __syncthreads_count(inside);  // (at most a block per thread: see the launch)
 
     // ---- Warp: blocks first .. last - 1 of the range.
     const int first = count * wid / kR4Warps, last = count * (wid + 1) / kR4Warps;
     auto issue = [&](int x, int half, uint32_t slot) {  // (one lane)
-        const int4 d = desc[x];
-        const uint8_t *src = a.pool + (int64_t)d.x * a.page_stride + (int64_t)(d.y % a.Hkv) * a.head_stride + (half ? SM::kHalf : 0);
+        const uint8_t *src = a.pool + *reinterpret_cast<const int64_t *>(&desc[x]) + (half ? SM::kHalf : 0);
         ptx::mbar_expect_tx(bars + 8u * slot, SM::kHalf);
         ptx::bulk_load(ring + slot * SM::kHalf, src, SM::kHalf, bars + 8u * slot);
     };
     const int halves = 2 * (last - first);
-    if (lane < NH && lane < halves) issue(first + (lane >> 1), lane & 1, (uint32_t)lane);
-    __syncwarp();
+    if (lane == 0 && halves) issue(first, 0, 0);  // (the others behind it, so that all warps' first K come first)
 
     const Kv4Lane<D> at(lane);
     Kv4Query<D> q;
-    uint4 raw[D / 32];
     Kv4State<D> st;
     st.clear();
-    if (first < last) Kv4Query<D>::load(a, (uint32_t)desc[first].y, lane, raw);
     bool ok = true;
     uint32_t slot = 0, parity = 0;
     auto next_slot = [&] {
@@ -737,26 +813,28 @@ __global__ void __launch_bounds__(kR4Threads, 1) kv4_range_kernel(const Kv4Args 
     bool whole = false;     // ... and in the row
 #pragma unroll 1
     for (int x = first; x < last; ++x) {
-        const int4 d = desc[x];
-        const int n_keys = (int)((uint32_t)d.w >> 24) + 1, n = d.w & 0xffffff;
+        const int32_t row = desc[x].z, w = desc[x].w, left = w & 0xffffff, n_keys = (w >> 24 & 63) + 1;
         if (row_start) {
+            uint4 raw[D / 32];
+            Kv4Query<D>::load(a, (uint32_t)row, lane, raw);
             q.set(raw, a.scale_log2, lane);
-            whole = d.z == n;
+            whole = w >> 30;
             row_start = false;
-            if (x + d.z < last) Kv4Query<D>::load(a, (uint32_t)desc[x + d.z].y, lane, raw);  // the next row's
+            if (x == first) {
+                if (lane > 0 && lane < NH && lane < halves) issue(first + (lane >> 1), lane & 1, (uint32_t)lane);
+                __syncwarp();
+            }
         }
         wait_half(1);
         if (!ok) break;
+        const bool partial = n_keys < kKv4Page;
         float sx[4][4];
         const uint32_t k_half = ring + slot * SM::kHalf;
 #pragma unroll
         for (int tile = 0; tile < 4; ++tile) {
-            if (16 * tile < n_keys) {
+            if (!partial || 16 * tile < n_keys) {
                 kv4_logits<D>(k_half, tile, at, q, sx[tile]);
-                if (n_keys < kKv4Page) {
-                    if (16 * tile + at.key >= n_keys) sx[tile][0] = sx[tile][1] = -INFINITY;
-                    if (16 * tile + at.key + 8 >= n_keys) sx[tile][2] = sx[tile][3] = -INFINITY;
-                }
+                kv4_mask(sx[tile], at.key, partial, n_keys - 16 * tile);
             } else {
                 sx[tile][0] = sx[tile][1] = sx[tile][2] = sx[tile][3] = -INFINITY;
             }
@@ -769,21 +847,20 @@ __global__ void __launch_bounds__(kR4Threads, 1) kv4_range_kernel(const Kv4Args 
             mx0 = fmaxf(mx0, fmaxf(sx[tile][0], sx[tile][2]));
             mx1 = fmaxf(mx1, fmaxf(sx[tile][1], sx[tile][3]));
         }
-        st.raise(mx0, mx1);
+        st.raise(mx0, mx1, q);
         wait_half(2);
         if (!ok) break;
         const uint32_t v_half = ring + slot * SM::kHalf;
 #pragma unroll
         for (int tile = 0; tile < 4; ++tile)
-            if (16 * tile < n_keys) {
+            if (!partial || 16 * tile < n_keys) {
                 float p[4];
-                const bool none_a = 16 * tile + at.key >= n_keys, none_b = 16 * tile + at.key + 8 >= n_keys;
-                st.weigh(sx[tile], none_a, none_b, p);
-                kv4_values<D, kF32>(v_half, tile, at, p, none_a, none_b, st.acc);
+                st.weigh(sx[tile], q, at.key, partial, n_keys - 16 * tile, p);
+                kv4_values<D, kF32>(v_half, tile, at, p, partial, n_keys - 16 * tile, st.acc);
             }
         refill(2 * (x - first) + 1 + NH);
         next_slot();
-        if (d.z == 1 && x + 1 < last) {  // the row ends, the range goes on
+        if (left == 1 && x + 1 < last) {  // the row ends, the range goes on
             st.sum_up();
             if (whole) {
                 const int g = lane >> 2, t = lane & 3;
@@ -791,7 +868,7 @@ __global__ void __launch_bounds__(kR4Threads, 1) kv4_range_kernel(const Kv4Args 
                 for (int y = 0; y < 2; ++y) {
                     const int h = 2 * t + y;
                     if (h < G) {
-                        const int64_t head = (int64_t)d.y * G + h;
+                        const int64_t head = (int64_t)row * G + h;
                         const float m = y ? st.m1 : st.m0, l = y ? st.l1 : st.l0, inv = 1.0f / l;
 #pragma unroll
                         for (int j = 0; j < D / 32; ++j)
@@ -803,7 +880,7 @@ __global__ void __launch_bounds__(kR4Threads, 1) kv4_range_kernel(const Kv4Args 
             } else {  // (only the range's first row can be this)
                 const uint32_t piece = smem + SM::kFirst + (uint32_t)wid * SM::kPiece;
                 st.store(piece, piece + kD4MaxGroup * SM::kRow, lane);
-                if (lane == 0) ids[2 * wid] = d.y;
+                if (lane == 0) ids[2 * wid] = row;
             }
             st.clear();
             row_start = true;
@@ -814,7 +891,7 @@ __global__ void __launch_bounds__(kR4Threads, 1) kv4_range_kernel(const Kv4Args 
     if (first < last && ok) {
         st.sum_up();
         st.store(ring, ring + kD4MaxGroup * SM::kRow, lane);
-        if (lane == 0) ids[2 * wid + 1] = desc[last - 1].y;
+        if (lane == 0) ids[2 * wid + 1] = desc[last - 1].z;
     }
     __syncthreads();
     if (*abort_flag) {
@@ -826,104 +903,164 @@ __global__ void __launch_bounds__(kR4Threads, 1) kv4_range_kernel(const Kv4Args 
         return;
     }
 
-    // ---- Pieces of the same row follow one another.  Warp: every twelfth run of them.
+    // ---- Pieces of the same row follow one another: a run of them.  Warp: a run, or where there are few, some heads of one.
     float *parts = a.parts + (int64_t)blockIdx.x * 2 * Kv4Part<D>::kFloats;
-    const int32_t row_first = count ? desc[0].y : -1, row_last = count ? desc[count - 1].y : -1;
-    const bool open_first = count && desc[0].z != (desc[0].w & 0xffffff), open_last = count && desc[count - 1].z != 1;
-    int run = 0;
-    for (int x = 0; x < 2 * kR4Warps;) {
-        const int32_t row = ids[x];
-        if (row < 0) {
-            ++x;
-            continue;
+    const int32_t row_first = count ? desc[0].z : -1, row_last = count ? desc[count - 1].z : -1;
+    const bool open_first = count && !(desc[0].w >> 30), open_last = count && (desc[count - 1].w & 0xffffff) != 1;
+    static_assert(2 * kR4Warps <= 32, "a lane per piece");
+    const int32_t id = lane < 2 * kR4Warps ? ids[lane] : -1;
+    const uint32_t valid = __ballot_sync(0xffffffffu, id >= 0), below = valid & ((1u << lane) - 1u);
+    const int32_t id_before = __shfl_sync(0xffffffffu, id, below ? 31 - __clz(below) : 0);
+    const uint32_t starts = __ballot_sync(0xffffffffu, id >= 0 && (below == 0 || id_before != id));
+    auto merge = [&](auto heads_of, int unit, int split) {  // heads unit % split, + split, ... of run unit / split
+        constexpr int NHd = decltype(heads_of)::value;
+        uint32_t rest = starts;
+        for (int run = unit / split; run > 0; --run) rest &= rest - 1;
+        const int h0 = unit % split, from = __ffs(rest) - 1;
+        const uint32_t more = rest & (rest - 1);
+        const uint32_t mask = valid & ~((1u << from) - 1u) & (more ? (1u << (__ffs(more) - 1)) - 1u : 0xffffffffu);
+        const int32_t row = __shfl_sync(0xffffffffu, id, from);
+        auto piece = [&](int y) { return y & 1 ? smem + (uint32_t)(y >> 1) * SM::kRing : smem + SM::kFirst + (uint32_t)(y >> 1) * SM::kPiece; };
+        // Lane: one piece's maxima and sums, then its weights.
+        const bool have = mask >> lane & 1u;
+        float m[NHd], l[NHd], w[NHd];
+        float4 out[NHd];
+#pragma unroll
+        for (int y = 0; y < NHd; ++y) {
+            m[y] = -INFINITY;
+            l[y] = 0.f;
+            if (have && h0 + split * y < kD4MaxGroup) ptx::ld_shared_v2(piece(lane) + kD4MaxGroup * SM::kRow + 8u * (h0 + split * y), m[y], l[y]);
+            w[y] = m[y];
+            out[y] = make_float4(0.f, 0.f, 0.f, 0.f);
         }
-        int end = x + 1;
-        while (end < 2 * kR4Warps && (ids[end] == row || ids[end] < 0)) ++end;
-        if (run++ % kR4Warps == wid) {
-            // A row that began in an earlier CTA is part 0, one that goes on in the next CTA part 1 (part 0 if both).
-            const bool from_before = open_first && row == row_first, goes_on = open_last && row == row_last;
-            float *part = from_before ? parts : goes_on ? parts + Kv4Part<D>::kFloats : nullptr;
-            for (int h = 0; h < G; ++h) {
-                float m = -INFINITY, l = 0.f;
-                float4 out = make_float4(0.f, 0.f, 0.f, 0.f);
-                auto piece = [&](int y) { return y & 1 ? smem + (uint32_t)(y >> 1) * SM::kRing : smem + SM::kFirst + (uint32_t)(y >> 1) * SM::kPiece; };
-                for (int y = x; y < end; ++y) {
-                    if (ids[y] != row) continue;
-                    float mp, lp;
-                    ptx::ld_shared_v2(piece(y) + kD4MaxGroup * SM::kRow + 8u * h, mp, lp);
-                    m = fmaxf(m, mp);
-                }
-                for (int y = x; y < end; ++y) {
-                    if (ids[y] != row) continue;
-                    float mp, lp;
-                    ptx::ld_shared_v2(piece(y) + kD4MaxGroup * SM::kRow + 8u * h, mp, lp);
-                    const float w = mp != -INFINITY ? ptx::ex2(mp - m) : 0.f;
-                    l = fmaf(lp, w, l);
-                    if (4 * lane < D) {
-                        float4 v;
-                        ptx::ld_shared_v4(piece(y) + (uint32_t)h * SM::kRow + 16u * lane, v.x, v.y, v.z, v.w);
-                        add_part(out, v, w);
-                    }
-                }
-                if (part) {
-                    if (4 * lane < D) *reinterpret_cast<float4 *>(part + 4 + 2 * kD4MaxGroup + h * D + 4 * lane) = out;
-                    if (lane == 0) *reinterpret_cast<float2 *>(part + 4 + 2 * h) = make_float2(m, l);
-                } else {
-                    const int64_t head = (int64_t)row * G + h;
-                    if (4 * lane < D) write4<kF32>(a.o, head * D + 4 * lane, out, 1.0f / l);
-                    if (lane == 0) a.lse[head] = natural(m, l);
+#pragma unroll
+        for (int o = 16; o > 0; o /= 2)
+#pragma unroll
+            for (int y = 0; y < NHd; ++y) m[y] = fmaxf(m[y], __shfl_xor_sync(0xffffffffu, m[y], o));
+#pragma unroll
+        for (int y = 0; y < NHd; ++y) {
+            w[y] = w[y] != -INFINITY ? ptx::ex2(w[y] - m[y]) : 0.f;
+            l[y] *= w[y];
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o /= 2)
+#pragma unroll
+            for (int y = 0; y < NHd; ++y) l[y] += __shfl_xor_sync(0xffffffffu, l[y], o);
+        for (uint32_t left = mask; left; left &= left - 1) {
+            const int p = __ffs(left) - 1;
+#pragma unroll
+            for (int y = 0; y < NHd; ++y) {
+                const float wy = __shfl_sync(0xffffffffu, w[y], p);
+                if (4 * lane < D && h0 + split * y < G) {
+                    float4 v;
+                    ptx::ld_shared_v4(piece(p) + (uint32_t)(h0 + split * y) * SM::kRow + 16u * lane, v.x, v.y, v.z, v.w);
+                    add_part(out[y], v, wy);
                 }
             }
         }
-        x = end;
-    }
-    if (tid < 2) {
+        // A row that began in an earlier CTA is part 0, one that goes on in the next CTA part 1 (part 0 if both).
+        const bool from_before = open_first && row == row_first, goes_on = open_last && row == row_last;
+        float *part = parts + (from_before ? 0 : Kv4Part<D>::kFloats);
+#pragma unroll
+        for (int y = 0; y < NHd; ++y) {
+            const int h = h0 + split * y;
+            if (h >= G) break;
+            if (from_before || goes_on) {
+                if (4 * lane < D) *reinterpret_cast<float4 *>(part + 4 + 2 * kD4MaxGroup + h * D + 4 * lane) = out[y];
+                if (lane == 0) *reinterpret_cast<float2 *>(part + 4 + 2 * h) = make_float2(m[y], l[y]);
+            } else {
+                const int64_t head = (int64_t)row * G + h;
+                if (4 * lane < D) write4<kF32>(a.o, head * D + 4 * lane, out[y], 1.0f / l[y]);
+                if (lane == 0) a.lse[head] = natural(m[y], l[y]);
+            }
+        }
+    };
+    const int runs = __popc(starts);
+    if (4 * runs > kR4Warps)
+        for (int unit = wid; unit < runs; unit += kR4Warps) merge(std::integral_constant<int, kD4MaxGroup>(), unit, 1);
+    else if (wid < 4 * runs)
+        merge(std::integral_constant<int, 2>(), wid, 4);
+    if (tid < 2 && !a.whole_rows) {
         const bool there = tid == 0 ? open_first : open_last && !(open_first && row_first == row_last);
         reinterpret_cast<int32_t *>(parts + tid * Kv4Part<D>::kFloats)[0] = there ? (tid == 0 ? row_first : row_last) : count ? -1 : -2;
     }
 
     // ---- Sequences without a key (a length outside [1, max_len]): zeros.
     for (int b = blockIdx.x; b < a.batch; b += gridDim.x) {
-        int32_t len;
-        if (row_of(b, len).n) continue;
+        if (len_of(b)) continue;
         const int heads = a.Hkv * G;
         for (int x = tid; x < heads * D / 4; x += kR4Threads) write4<kF32>(a.o, (int64_t)b * heads * D + 4 * x, make_float4(0.f, 0.f, 0.f, 0.f), 0.f);
         for (int x = tid; x < heads; x += kR4Threads) a.lse[(int64_t)b * heads + x] = -INFINITY;
     }
 }
 
-// Rows that more than one CTA of kv4_range_kernel has a part of: the CTA whose last row goes on in the next ones.  A warp a head.
+// Rows that more than one CTA of kv4_range_kernel has a part of: the CTA whose last row goes on in the next ones.  Warp: heads h
+// and h + 4; lane: four features.  Small, so that its CTAs wait beside those of the range kernel.
+constexpr int kJ4Threads = 128;
+
 template <int D, bool kF32>
-__global__ void __launch_bounds__(32 * kD4MaxGroup) kv4_join_kernel(const Kv4Args a)
+__global__ void __launch_bounds__(kJ4Threads) kv4_join_kernel(const Kv4Args a)
 {
-    const int lane = threadIdx.x & 31, h = threadIdx.x >> 5;
+    constexpr int64_t kStep = 2 * Kv4Part<D>::kFloats;  // from one CTA's parts to the next one's
+    const int lane = threadIdx.x & 31;
+    const unsigned c0 = blockIdx.x;
+    const float *part = a.parts + (int64_t)c0 * kStep + Kv4Part<D>::kFloats, *next = a.parts + (int64_t)(c0 + 1) * kStep;
     pdl_launch_next();
     pdl_wait();
-    const float *part = a.parts + ((int64_t)blockIdx.x * 2 + 1) * Kv4Part<D>::kFloats;
     const int32_t row = *reinterpret_cast<const int32_t *>(part);
-    if (row < 0 || h >= a.G) return;
-    // Its other parts: part 0 of the next CTAs that have blocks.
-    float m = part[4 + 2 * h], l = part[5 + 2 * h];
-    float4 out = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (4 * lane < D) out = *reinterpret_cast<const float4 *>(part + 4 + 2 * kD4MaxGroup + h * D + 4 * lane);
-    for (unsigned c = blockIdx.x + 1; c < gridDim.x; ++c) {
-        const float *next = a.parts + (int64_t)c * 2 * Kv4Part<D>::kFloats;
-        const int32_t id = *reinterpret_cast<const int32_t *>(next);
-        if (id == -2) continue;
-        if (id != row) break;
-        const float2 s = *reinterpret_cast<const float2 *>(next + 4 + 2 * h);
-        const float top = fmaxf(m, s.x);  // (no number: a part whose logits are all NaN, as its sum)
-        const float w0 = m != -INFINITY ? ptx::ex2(m - top) : 0.f, w1 = s.x != -INFINITY ? ptx::ex2(s.x - top) : 0.f;
-        m = top;
-        l = l * w0 + s.y * w1;
-        if (4 * lane < D) {
+    // Its other parts are part 0 of the next CTAs that have blocks.  Lane: one of these CTAs.
+    unsigned first = 0;
+    auto look = [&](uint32_t &mask) {  // which of the next 32 have a part; whether the row ends among them
+        const unsigned c = c0 + 1 + first + lane;
+        const int32_t id = c < gridDim.x ? *reinterpret_cast<const int32_t *>(next + (int64_t)(first + lane) * kStep) : -1;
+        const uint32_t others = __ballot_sync(0xffffffffu, id != row && id != -2);
+        const uint32_t until = others ? (1u << (__ffs(others) - 1)) - 1u : 0xffffffffu;
+        mask = __ballot_sync(0xffffffffu, id == row) & until;
+        return others != 0;
+    };
+    uint32_t mask;
+    bool ends = look(mask);
+    if (row < 0) return;
+    for (int h = threadIdx.x >> 5; h < a.G; h += kJ4Threads / 32) {
+        float m = part[4 + 2 * h], l = part[5 + 2 * h];
+        float4 out = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (4 * lane < D) out = *reinterpret_cast<const float4 *>(part + 4 + 2 * kD4MaxGroup + h * D + 4 * lane);
+        while (true) {
+            const float *mine = next + (int64_t)(first + lane) * kStep;
+            float mp = -INFINITY, lp = 0.f;
+            if (mask >> lane & 1u) {
+                mp = mine[4 + 2 * h];
+                lp = mine[5 + 2 * h];
+            }
+            float top = mp;
+#pragma unroll
+            for (int o = 16; o > 0; o /= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+            top = fmaxf(top, m);
+            const float w0 = m != -INFINITY ? ptx::ex2(m - top) : 0.f, w = mp != -INFINITY ? ptx::ex2(mp - top) : 0.f;
+            lp *= w;
+#pragma unroll
+            for (int o = 16; o > 0; o /= 2) lp += __shfl_xor_sync(0xffffffffu, lp, o);
+            l = fmaf(l, w0, lp);
+            m = top;
             out = make_float4(out.x * w0, out.y * w0, out.z * w0, out.w * w0);
-            add_part(out, *reinterpret_cast<const float4 *>(next + 4 + 2 * kD4MaxGroup + h * D + 4 * lane), w1);
+            for (uint32_t left = mask; left; left &= left - 1) {
+                const int p = __ffs(left) - 1;
+                const float wp = __shfl_sync(0xffffffffu, w, p);
+                if (4 * lane < D)
+                    add_part(out, *reinterpret_cast<const float4 *>(next + (int64_t)(first + p) * kStep + 4 + 2 * kD4MaxGroup + h * D + 4 * lane), wp);
+            }
+            if (ends) break;
+            first += 32;
+            ends = look(mask);
+        }
+        const int64_t head = (int64_t)row * a.G + h;
+        if (4 * lane < D) write4<kF32>(a.o, head * D + 4 * lane, out, 1.0f / l);
+        if (lane == 0) a.lse[head] = natural(m, l);
+        if (first) {  // (a row of more than 33 CTAs: the next head begins with the first ones again)
+            first = 0;
+            ends = look(mask);
         }
     }
-    const int64_t head = (int64_t)row * a.G + h;
-    if (4 * lane < D) write4<kF32>(a.o, head * D + 4 * lane, out, 1.0f / l);
-    if (lane == 0) a.lse[head] = natural(m, l);
 }
 
 // ------------------------------------------------------------------------------------------ host
@@ -959,11 +1096,17 @@ static pa_status check_kv4(const pa_kv4_params *p)
     return PA_OK;
 }
 
-// CTAs of the range kernel: no range is longer than a block per thread, whatever the lengths are.
+// Whether ranges are rounded to whole rows: where a row is worth less than the second kernel, and CTAs have many.
+static bool kv4_whole_rows(const pa_kv4_params *p)
+{
+    return kv4_most_blocks(p) <= 24 && (int64_t)p->batch * p->pool.n_kv_heads >= 2 * kR4Ctas;
+}
+// CTAs of the range kernel: no range, rounded or not, is longer than a block per thread, whatever the lengths are.
 static int64_t kv4_range_ctas(const pa_kv4_params *p)
 {
-    const int64_t blocks = (int64_t)p->batch * p->pool.n_kv_heads * kv4_most_blocks(p);
-    const int64_t turns = (blocks + (int64_t)kR4Ctas * kR4Threads - 1) / ((int64_t)kR4Ctas * kR4Threads);
+    const int64_t most = kv4_most_blocks(p), blocks = (int64_t)p->batch * p->pool.n_kv_heads * most;
+    const int64_t room = kv4_whole_rows(p) ? kR4Threads - 2 * most : kR4Threads;
+    const int64_t turns = (blocks + kR4Ctas * room - 1) / (kR4Ctas * room);
     return turns * kR4Ctas;
 }
 
@@ -1120,9 +1263,10 @@ extern "C" pa_status pa_decode_kv4(const pa_kv4_params *p, const void *q, const 
     }
     a.R = 1;
     a.stages = 0;
+    a.whole_rows = kv4_whole_rows(p);
     const unsigned ctas = (unsigned)kv4_range_ctas(p);
     const size_t smem = D == 128 ? Kv4RangeSmem<128>::bytes() : Kv4RangeSmem<64>::bytes();
     PA_CUDA_OK(launch_pdl(kv4_kernel(D, f32, 1), dim3(ctas), kR4Threads, smem, st, a));
-    PA_CUDA_OK(launch_pdl(kv4_kernel(D, f32, 2), dim3(ctas), 32 * kD4MaxGroup, 0, st, a));
+    if (!a.whole_rows) PA_CUDA_OK(launch_pdl(kv4_kernel(D, f32, 2), dim3(ctas), kJ4Threads, 0, st, a));
     return PA_OK;
 }

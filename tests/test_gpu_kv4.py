@@ -138,11 +138,11 @@ def _near(o, lse, ref, o_dtype):
     A logit: exact products, 128 of them summed in fp32 (tensor cores: at most 2^-23 of the running sum a step, of the terms'
     sum L 2^-18 at most, taken as 2^-19 L over the four groups' chains of eight), scales and factors 2^-22 L: its weight is off by
     that in relative terms, plus ex2.approx and the sums of weights (4 x 2^-22 and 2^-19).  Twice for the quotient.  Weights for bf16 outputs
-    are rounded to bf16, 2^-8; for fp32 outputs in two parts, 2^-16.  The output's rounding: 2^-8."""
+    are rounded to bf16, 2^-8, and times their scale once more, (1 + 2^-8)^2 - 1 < 2^-7 + 2^-15; for fp32 outputs in two parts, 2^-16.  The output's rounding: 2^-8."""
     ref_o, ref_lse, size, most = (x.to(o.device) for x in ref)
     logit = 2.0 ** -18 * most + 2.0 ** -18
     assert ((lse.double() - ref_lse).abs() <= logit + ref_lse.abs() * 2.0 ** -22).all(), float(((lse.double() - ref_lse).abs() / logit).max())
-    weight = 2 * logit + (2.0 ** -8 if o_dtype == torch.bfloat16 else 2.0 ** -16)
+    weight = 2 * logit + (2.0 ** -7 + 2.0 ** -15 if o_dtype == torch.bfloat16 else 2.0 ** -16)
     bound = weight[:, None] * size + (ref_o.abs() * 2.0 ** -8 if o_dtype == torch.bfloat16 else 0) + 1e-30
     err = (o.double() - ref_o).abs()
     assert torch.isfinite(o.float()).all()
