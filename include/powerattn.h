@@ -398,7 +398,7 @@ pa_status pa_build_block_tables(const pa_table_params *p, const int32_t *new_len
 typedef struct {
     int32_t batch, n_q_heads, n_kv_heads, head_dim; /* head_dim in {64, 128}                   */
     int64_t seq_len;                                /* tokens of a batch entry                 */
-    int32_t rotary_dim;                             /* a multiple of 8, in [0, head_dim]       */
+    int32_t rotary_dim;                             /* a multiple of 16, in [0, head_dim]      */
     int32_t interleaved;                            /* 0: pairs (i, i + rotary_dim / 2)        */
     int32_t max_positions;                          /* rows of cos_sin                         */
     float eps;                                      /* >= 0                                    */

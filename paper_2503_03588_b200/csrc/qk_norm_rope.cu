@@ -2,18 +2,21 @@
 // token's position, in one pass over both tensors.
 //
 // Bound by memory: a head is read and written once (backward: the head, its output's gradient, its gradient).  D / 8 lanes
-// share a head, eight features each, as two pieces of four that belong together under the rotation, so that nothing but the
-// norm's sums crosses lanes.  A warp works on 256 / D heads of one token at a time and keeps the token's cosines and sines and
-// the weights in registers over all of the token's heads.
+// share a head, eight features each: four pairs that belong together under the rotation, so that nothing but the norm's sums
+// crosses lanes.  A warp works on 256 / D heads of one token at a time, two numbers an instruction, and keeps what the token's heads share
+// in registers.
 #include <cuda_bf16.h>
 #include <math.h>
 
 #include "common.cuh"
+#include "sm100_ptx.cuh"
 
 namespace pa {
 
-constexpr int kRopeThreads = 256;
+constexpr int kRopeThreads = 128;
 constexpr int kRopeWarps = kRopeThreads / 32;
+constexpr int kBackThreads = 256;
+constexpr int kBackWarps = kBackThreads / 32;
 
 struct RopeArgs {
     const __nv_bfloat16 *q, *k;
@@ -26,82 +29,105 @@ struct RopeArgs {
     pa_strides sq, sk, sqo, sko;            // (backward: sqo, sko are those of d_q, d_k)
     int64_t tokens, seq;                    // of all batch entries, of one
     int32_t Hq, Hkv, half, max_positions;   // half: pairs that are rotated
-    int32_t interleaved, w_f32, chunks, heads_per_chunk;
+    int32_t w_f32, chunks;
     float eps;
 };
 
-__device__ __forceinline__ uint2 ld8(const void *p) { return *reinterpret_cast<const uint2 *>(p); }
-__device__ __forceinline__ void unpack4(const uint2 &u, float *x)
-{
-    x[0] = __uint_as_float(u.x << 16);
-    x[1] = __uint_as_float(u.x & 0xffff0000u);
-    x[2] = __uint_as_float(u.y << 16);
-    x[3] = __uint_as_float(u.y & 0xffff0000u);
-}
-__device__ __forceinline__ uint32_t pack2(float lo, float hi)
-{
-    const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
-    return *reinterpret_cast<const uint32_t *>(&h);
-}
-__device__ __forceinline__ uint2 pack4(const float *x) { return make_uint2(pack2(x[0], x[1]), pack2(x[2], x[3])); }
+using ptx::add_f32x2;
+using ptx::fma_f32x2;
+using ptx::mul_f32x2;
+using ptx::pack_f32x2;
 
-// Where a lane's two pieces of four features stand in a head, and the first of its four angles.
+// Eight numbers of a lane as four pairs: [0], [1] hold the first numbers of its four rotated pairs, [2], [3] the second ones.
+struct Eight {
+    uint64_t v[4];
+};
+__device__ __forceinline__ uint64_t both(float x) { return pack_f32x2(x, x); }
+__device__ __forceinline__ float bf_lo(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float bf_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
+// A lane's pieces of four features, a and b, in that order and back.  In neighbouring pairs (kPairs) the pieces hold first and
+// second numbers in turns, else piece a the first and piece b the second ones.
+template <bool kPairs>
+__device__ __forceinline__ Eight in_order(float a0, float a1, float a2, float a3, float b0, float b1, float b2, float b3)
+{
+    if (kPairs) return {{pack_f32x2(a0, a2), pack_f32x2(b0, b2), pack_f32x2(a1, a3), pack_f32x2(b1, b3)}};
+    return {{pack_f32x2(a0, a1), pack_f32x2(a2, a3), pack_f32x2(b0, b1), pack_f32x2(b2, b3)}};
+}
+template <bool kPairs>
+__device__ __forceinline__ Eight from_bf16(const uint2 &a, const uint2 &b)
+{
+    return in_order<kPairs>(bf_lo(a.x), bf_hi(a.x), bf_lo(a.y), bf_hi(a.y), bf_lo(b.x), bf_hi(b.x), bf_lo(b.y), bf_hi(b.y));
+}
+template <bool kPairs>
+__device__ __forceinline__ void pieces(const Eight &e, float (&x)[8])
+{
+    float f0, f1, f2, f3, s0, s1, s2, s3;
+    ptx::unpack_f32x2(e.v[0], f0, f1);
+    ptx::unpack_f32x2(e.v[1], f2, f3);
+    ptx::unpack_f32x2(e.v[2], s0, s1);
+    ptx::unpack_f32x2(e.v[3], s2, s3);
+    if (kPairs) {
+        x[0] = f0; x[1] = s0; x[2] = f1; x[3] = s1;
+        x[4] = f2; x[5] = s2; x[6] = f3; x[7] = s3;
+    } else {
+        x[0] = f0; x[1] = f1; x[2] = f2; x[3] = f3;
+        x[4] = s0; x[5] = s1; x[6] = s2; x[7] = s3;
+    }
+}
+template <bool kPairs>
+__device__ __forceinline__ void write_bf16(const Eight &e, __nv_bfloat16 *a, __nv_bfloat16 *b)
+{
+    float x[8];
+    pieces<kPairs>(e, x);
+    *reinterpret_cast<uint2 *>(a) = make_uint2(ptx::cvt_bf16x2(x[0], x[1]), ptx::cvt_bf16x2(x[2], x[3]));
+    *reinterpret_cast<uint2 *>(b) = make_uint2(ptx::cvt_bf16x2(x[4], x[5]), ptx::cvt_bf16x2(x[6], x[7]));
+}
+__device__ __forceinline__ uint2 ld8(const void *p) { return *reinterpret_cast<const uint2 *>(p); }
+
+// Where a lane's pieces stand in a head, and the first of its four angles.  Rotated features in halves: the lane's first numbers
+// in piece a, their partners half a rotated part further on; else eight neighbours.
 struct Pieces {
     int a, b, angle;
     bool rotated;
 };
-__device__ __forceinline__ Pieces pieces_of(int l, int half, bool interleaved)
+template <bool kPairs>
+__device__ __forceinline__ Pieces pieces_of(int l, int half)
 {
     Pieces p;
     p.angle = 4 * l;
     p.rotated = 4 * l < half;
-    // (behind the rotated features, 2 half + 8 (l - half / 4) = 8 l)
-    p.a = !interleaved && p.rotated ? 4 * l : 8 * l;
-    p.b = !interleaved && p.rotated ? half + 4 * l : 8 * l + 4;
+    p.a = !kPairs && p.rotated ? 4 * l : 8 * l;
+    p.b = !kPairs && p.rotated ? half + 4 * l : 8 * l + 4;
     return p;
 }
-// x[0..3] is piece a, x[4..7] piece b.
-__device__ __forceinline__ void rotate(float *x, const float *c, const float *s, bool interleaved)
+template <bool kPairs, typename T>
+__device__ __forceinline__ Eight load_eight(const T *src, const Pieces &p)
 {
-    if (interleaved) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float u = x[2 * i], v = x[2 * i + 1];
-            x[2 * i] = u * c[i] - v * s[i];
-            x[2 * i + 1] = v * c[i] + u * s[i];
-        }
+    if constexpr (sizeof(T) == 4) {
+        const float4 a = *reinterpret_cast<const float4 *>(src + p.a), b = *reinterpret_cast<const float4 *>(src + p.b);
+        return in_order<kPairs>(a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w);
     } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float u = x[i], v = x[4 + i];
-            x[i] = u * c[i] - v * s[i];
-            x[4 + i] = v * c[i] + u * s[i];
-        }
+        return from_bf16<kPairs>(ld8(src + p.a), ld8(src + p.b));
     }
 }
-__device__ __forceinline__ void load_weights(const void *w, bool f32, const Pieces &p, float *out)
+template <bool kPairs>
+__device__ __forceinline__ Eight load_weights(const void *w, bool f32, const Pieces &p)
 {
-    if (f32) {
-        const float4 a = *reinterpret_cast<const float4 *>(static_cast<const float *>(w) + p.a);
-        const float4 b = *reinterpret_cast<const float4 *>(static_cast<const float *>(w) + p.b);
-        out[0] = a.x; out[1] = a.y; out[2] = a.z; out[3] = a.w;
-        out[4] = b.x; out[5] = b.y; out[6] = b.z; out[7] = b.w;
-    } else {
-        unpack4(ld8(static_cast<const __nv_bfloat16 *>(w) + p.a), out);
-        unpack4(ld8(static_cast<const __nv_bfloat16 *>(w) + p.b), out + 4);
-    }
+    return f32 ? load_eight<kPairs>(static_cast<const float *>(w), p) : load_eight<kPairs>(static_cast<const __nv_bfloat16 *>(w), p);
 }
-// The four angles of a token.
-__device__ __forceinline__ void load_angles(const RopeArgs &a, const Pieces &p, int32_t pos, float *c, float *s)
+// The cosines and sines of a token's four pairs (not rotated: 1 and 0).
+struct Angles {
+    uint64_t c[2], s[2];
+};
+__device__ __forceinline__ Angles load_angles(const RopeArgs &a, const Pieces &p, int32_t pos)
 {
-    float4 u = make_float4(0.f, 0.f, 0.f, 0.f), v = u;
+    float4 u = make_float4(1.f, 1.f, 1.f, 1.f), v = make_float4(0.f, 0.f, 0.f, 0.f);
     if (p.rotated) {
         const float *row = a.cos_sin + (int64_t)pos * (2 * a.half) + p.angle;
         u = *reinterpret_cast<const float4 *>(row);
         v = *reinterpret_cast<const float4 *>(row + a.half);
     }
-    c[0] = u.x; c[1] = u.y; c[2] = u.z; c[3] = u.w;
-    s[0] = v.x; s[1] = v.y; s[2] = v.z; s[3] = v.w;
+    return {{pack_f32x2(u.x, u.y), pack_f32x2(u.z, u.w)}, {pack_f32x2(v.x, v.y), pack_f32x2(v.z, v.w)}};
 }
 template <int kLanes>
 __device__ __forceinline__ float sum_lanes(float x)
@@ -110,170 +136,311 @@ __device__ __forceinline__ float sum_lanes(float x)
     for (int o = kLanes / 2; o > 0; o /= 2) x += __shfl_xor_sync(0xffffffffu, x, o);
     return x;
 }
+__device__ __forceinline__ float sum_pairs(uint64_t x)
+{
+    float lo, hi;
+    ptx::unpack_f32x2(x, lo, hi);
+    return lo + hi;
+}
+__device__ __forceinline__ uint64_t negative(uint64_t x) { return x ^ 0x8000000080000000ull; }
 
-// A warp takes heads_per_chunk heads of a token, kBatch times 256 / D of them at a time.
-template <int D, int kBatch>
-__global__ void __launch_bounds__(kRopeThreads) rope_kernel(const RopeArgs a)
+// What a lane multiplies a head's numbers by, weights, cosines and sines once for all heads of a token:
+// out_first = r (first w c - second w s), out_second = r (second w c + first w s)
+struct Factors {
+    uint64_t fc[2], sc[2], fs[2], ss[2];
+};
+__device__ __forceinline__ Factors factors(const Eight &w, const Angles &t)
+{
+    Factors f;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        f.fc[i] = mul_f32x2(w.v[i], t.c[i]);
+        f.sc[i] = mul_f32x2(w.v[2 + i], t.c[i]);
+        f.fs[i] = mul_f32x2(w.v[i], t.s[i]);
+        f.ss[i] = negative(mul_f32x2(w.v[2 + i], t.s[i]));
+    }
+    return f;
+}
+// Numbers times r, multiplied and rotated.
+__device__ __forceinline__ Eight turned(const Eight &v, uint64_t r, const Factors &k, bool rotated)
+{
+    Eight o;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const uint64_t f = mul_f32x2(v.v[i], r), g = mul_f32x2(v.v[2 + i], r);
+        if (rotated) {
+            o.v[i] = fma_f32x2(f, k.fc[i], mul_f32x2(g, k.ss[i]));
+            o.v[2 + i] = fma_f32x2(g, k.sc[i], mul_f32x2(f, k.fs[i]));
+        } else {
+            o.v[i] = mul_f32x2(f, k.fc[i]);
+            o.v[2 + i] = mul_f32x2(g, k.sc[i]);
+        }
+    }
+    return o;
+}
+
+// Forward, few tokens: a warp takes 256 / D heads of a token, so that the call is as short as one chain of loads.
+template <int D, bool kPairs>
+__global__ void __launch_bounds__(kRopeThreads) rope_few_kernel(const RopeArgs a)
 {
     constexpr int kLanes = D / 8, kHeads = 32 / kLanes;
     pdl_launch_next();
     const int lane = threadIdx.x & 31, l = lane % kLanes, mine = lane / kLanes;
-    const Pieces p = pieces_of(l, a.half, a.interleaved);
-    const int64_t item = (int64_t)blockIdx.x * kRopeWarps + (threadIdx.x >> 5);
-    const int64_t token = item / a.chunks;
-    const int chunk = (int)(item - token * a.chunks);
+    const Pieces p = pieces_of<kPairs>(l, a.half);
+    const int64_t item = (int64_t)blockIdx.x * kRopeWarps + (threadIdx.x >> 5), token = item / a.chunks;
+    const int h0 = (int)(item - token * a.chunks) * kHeads + mine, q_chunks = (a.Hq + kHeads - 1) / kHeads * kHeads;
+    const bool is_k = h0 - mine >= q_chunks;
+    const int h = is_k ? h0 - q_chunks : h0;
     pdl_wait();
     if (token >= a.tokens) return;
     const int32_t pos = a.positions[token];
-    if (pos < 0 || pos >= a.max_positions) return;
     const int64_t b = token / a.seq, n = token - b * a.seq;
-    const __nv_bfloat16 *q = a.q + b * a.sq.batch + n * a.sq.seq, *k = a.k + b * a.sk.batch + n * a.sk.seq;
-    __nv_bfloat16 *q_out = a.q_out + b * a.sqo.batch + n * a.sqo.seq, *k_out = a.k_out + b * a.sko.batch + n * a.sko.seq;
-    float c[4], s[4], wq[8], wk[8];
-    load_angles(a, p, pos, c, s);
-    load_weights(a.q_weight, a.w_f32, p, wq);
-    load_weights(a.k_weight, a.w_f32, p, wk);
-    const int H = a.Hq + a.Hkv, first = chunk * a.heads_per_chunk;
-    const int end = first + a.heads_per_chunk < H ? first + a.heads_per_chunk : H;
-    for (int h0 = first; h0 < end; h0 += kBatch * kHeads) {
-        uint2 ra[kBatch], rb[kBatch];
+    const pa_strides &sx = is_k ? a.sk : a.sq, &so = is_k ? a.sko : a.sqo;
+    const bool in = h < (is_k ? a.Hkv : a.Hq);
+    const __nv_bfloat16 *x = (is_k ? a.k : a.q) + b * sx.batch + n * sx.seq + (in ? h : 0) * sx.head;
+    const uint2 ra = ld8(x + p.a), rb = ld8(x + p.b);
+    const Eight w = load_weights<kPairs>(is_k ? a.k_weight : a.q_weight, a.w_f32, p);
+    if (pos < 0 || pos >= a.max_positions) return;
+    __nv_bfloat16 *out = (is_k ? a.k_out : a.q_out) + b * so.batch + n * so.seq + (in ? h : 0) * so.head;
+    const Eight v = from_bf16<kPairs>(ra, rb);
+    uint64_t sq = 0;
 #pragma unroll
-        for (int x = 0; x < kBatch; ++x) {
-            const int h = h0 + x * kHeads + mine;
-            if (h < end) {
-                const __nv_bfloat16 *src = h < a.Hq ? q + h * a.sq.head : k + (h - a.Hq) * a.sk.head;
-                ra[x] = ld8(src + p.a);
-                rb[x] = ld8(src + p.b);
-            } else {
-                ra[x] = rb[x] = make_uint2(0u, 0u);
-            }
-        }
-#pragma unroll
-        for (int x = 0; x < kBatch; ++x) {
-            const int h = h0 + x * kHeads + mine;
-            float v[8];
-            unpack4(ra[x], v);
-            unpack4(rb[x], v + 4);
-            float sq = 0.f;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) sq = fmaf(v[i], v[i], sq);
-            const float r = rsqrtf(sum_lanes<kLanes>(sq) * (1.0f / D) + a.eps);
-            const bool is_q = h < a.Hq;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] *= r * (is_q ? wq[i] : wk[i]);
-            if (p.rotated) rotate(v, c, s, a.interleaved);
-            if (h < end) {
-                __nv_bfloat16 *dst = is_q ? q_out + h * a.sqo.head : k_out + (h - a.Hq) * a.sko.head;
-                *reinterpret_cast<uint2 *>(dst + p.a) = pack4(v);
-                *reinterpret_cast<uint2 *>(dst + p.b) = pack4(v + 4);
-            }
-        }
-    }
+    for (int i = 0; i < 4; ++i) sq = fma_f32x2(v.v[i], v.v[i], sq);
+    const uint64_t r = both(rsqrtf(sum_lanes<kLanes>(sum_pairs(sq)) * (1.0f / D) + a.eps));
+    if (in) write_bf16<kPairs>(turned(v, r, factors(w, load_angles(a, p, pos)), p.rotated), out + p.a, out + p.b);
 }
 
-template <typename T>
-__device__ __forceinline__ void load_gradient(const T *src, const Pieces &p, float *g)
+// Forward.  Warps stride over the tokens, 2 x 512 / D heads at a time; the next ones, of the next token too, are on their way while
+// these are worked on.  A lane has sixteen features here, two times eight numbers as above: half the instructions a head, of
+// which there were too many with eight (32K tokens, 28 / 4 heads: 100 us).
+template <int D, bool kPairs>
+__global__ void __launch_bounds__(kBackThreads, 2) rope_kernel(const RopeArgs a)
 {
-    if constexpr (sizeof(T) == 4) {
-        const float4 a = *reinterpret_cast<const float4 *>(src + p.a), b = *reinterpret_cast<const float4 *>(src + p.b);
-        g[0] = a.x; g[1] = a.y; g[2] = a.z; g[3] = a.w;
-        g[4] = b.x; g[5] = b.y; g[6] = b.z; g[7] = b.w;
-    } else {
-        unpack4(ld8(src + p.a), g);
-        unpack4(ld8(src + p.b), g + 4);
-    }
-}
-
-// Warps stride over the tokens and keep the weights' gradients in registers; at the end a CTA adds its warps' up, in their
-// order, and leaves the sums for rope_weights_kernel.
-template <int D, typename T>
-__global__ void __launch_bounds__(kRopeThreads) rope_backward_kernel(const RopeArgs a)
-{
-    constexpr int kLanes = D / 8, kHeads = 32 / kLanes, kBatch = 2;
-    __shared__ float sums[kRopeWarps * kHeads][2][D];
+    constexpr int kLanes = D / 16, kHeads = 32 / kLanes, kBatch = 2;
     pdl_launch_next();
     const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, l = lane % kLanes, mine = lane / kLanes;
-    const Pieces p = pieces_of(l, a.half, a.interleaved);
-    float dw[2][8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) dw[0][i] = dw[1][i] = 0.f;
+    const bool rotated = 8 * l < a.half;
+    const int pa = !kPairs && rotated ? 8 * l : 16 * l, pb = !kPairs && rotated ? a.half + 8 * l : 16 * l + 8;
+    const int64_t step = (int64_t)gridDim.x * kBackWarps;
     pdl_wait();
-    for (int64_t token = (int64_t)blockIdx.x * kRopeWarps + wid; token < a.tokens; token += (int64_t)gridDim.x * kRopeWarps) {
+    auto position = [&](int64_t token) {  // -1: none
+        const int32_t pos = token < a.tokens ? a.positions[token] : -1;
+        return pos < a.max_positions ? pos : -1;
+    };
+    auto place = [&](int64_t token, const pa_strides &s) {
+        const int64_t b = a.seq >= a.tokens ? 0 : token / a.seq;
+        return b * s.batch + (token - b * a.seq) * s.seq + mine * s.head;
+    };
+    uint4 ra[kBatch], rb[kBatch];
+    auto load = [&](const __nv_bfloat16 *x, int64_t x_step, int heads) {  // (heads from this lane's first one on)
+#pragma unroll
+        for (int y = 0; y < kBatch; ++y) {
+            ra[y] = rb[y] = make_uint4(0u, 0u, 0u, 0u);
+            if (y * kHeads < heads) {
+                ra[y] = *reinterpret_cast<const uint4 *>(x + pa);
+                rb[y] = *reinterpret_cast<const uint4 *>(x + pb);
+            }
+            x += x_step;
+        }
+    };
+    int64_t token = (int64_t)blockIdx.x * kBackWarps + wid;
+    if (token >= a.tokens) return;
+    int32_t pos = position(token), pos_next = position(token + step);
+    load(a.q + place(token, a.sq), kHeads * a.sq.head, a.Hq - mine);
+    for (; token < a.tokens; token += step) {
+        const int32_t pos_after = position(token + 2 * step);
+#pragma unroll 1
+        for (int which = 0; which < 2; ++which) {
+            const int H = which ? a.Hkv : a.Hq;
+            const pa_strides &sx = which ? a.sk : a.sq, &so = which ? a.sko : a.sqo;
+            const int64_t x_step = kHeads * sx.head, out_step = kHeads * so.head;
+            const __nv_bfloat16 *x = (which ? a.k : a.q) + place(token, sx);
+            __nv_bfloat16 *out = (which ? a.k_out : a.q_out) + place(token, so);
+            Factors f[2];
+            {
+                float c[8] = {1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f}, s[8] = {};
+                if (rotated) {
+                    const float *row = a.cos_sin + (int64_t)(pos < 0 ? 0 : pos) * (2 * a.half) + 8 * l;
+#pragma unroll
+                    for (int i = 0; i < 8; i += 4) {
+                        const float4 u = *reinterpret_cast<const float4 *>(row + i), v = *reinterpret_cast<const float4 *>(row + a.half + i);
+                        c[i] = u.x; c[i + 1] = u.y; c[i + 2] = u.z; c[i + 3] = u.w;
+                        s[i] = v.x; s[i + 1] = v.y; s[i + 2] = v.z; s[i + 3] = v.w;
+                    }
+                }
+                const void *w = which ? a.k_weight : a.q_weight;
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const Pieces p = {pa + 4 * e, pb + 4 * e, 0, rotated};
+                    const int i = kPairs ? 2 * e : 4 * e, j = kPairs ? 4 + 2 * e : 4 * e + 2;
+                    const Angles t = {{pack_f32x2(c[i], c[i + 1]), pack_f32x2(c[j], c[j + 1])},
+                                      {pack_f32x2(s[i], s[i + 1]), pack_f32x2(s[j], s[j + 1])}};
+                    f[e] = factors(load_weights<kPairs>(w, a.w_f32, p), t);
+                }
+            }
+            for (int h = 0; h < H; h += kBatch * kHeads) {
+                uint4 va[kBatch], vb[kBatch];
+#pragma unroll
+                for (int y = 0; y < kBatch; ++y) {
+                    va[y] = ra[y];
+                    vb[y] = rb[y];
+                }
+                x += kBatch * x_step;
+                if (h + kBatch * kHeads < H) load(x, x_step, H - mine - (h + kBatch * kHeads));
+                else if (which == 0) load(a.k + place(token, a.sk), kHeads * a.sk.head, a.Hkv - mine);
+                else if (token + step < a.tokens) load(a.q + place(token + step, a.sq), kHeads * a.sq.head, a.Hq - mine);
+#pragma unroll
+                for (int y = 0; y < kBatch; ++y) {
+                    Eight v[2] = {from_bf16<kPairs>(make_uint2(va[y].x, va[y].y), make_uint2(vb[y].x, vb[y].y)),
+                                  from_bf16<kPairs>(make_uint2(va[y].z, va[y].w), make_uint2(vb[y].z, vb[y].w))};
+                    uint64_t sq[2] = {0, 0};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        sq[0] = fma_f32x2(v[0].v[i], v[0].v[i], sq[0]);
+                        sq[1] = fma_f32x2(v[1].v[i], v[1].v[i], sq[1]);
+                    }
+                    const uint64_t r = both(rsqrtf(sum_lanes<kLanes>(sum_pairs(add_f32x2(sq[0], sq[1]))) * (1.0f / D) + a.eps));
+                    float o[2][8];
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) pieces<kPairs>(turned(v[e], r, f[e], rotated), o[e]);
+                    if (pos >= 0 && h + y * kHeads + mine < H) {
+                        auto four = [&](int i) {
+                            return make_uint4(ptx::cvt_bf16x2(o[0][i], o[0][i + 1]), ptx::cvt_bf16x2(o[0][i + 2], o[0][i + 3]),
+                                              ptx::cvt_bf16x2(o[1][i], o[1][i + 1]), ptx::cvt_bf16x2(o[1][i + 2], o[1][i + 3]));
+                        };
+                        *reinterpret_cast<uint4 *>(out + pa) = four(0);
+                        *reinterpret_cast<uint4 *>(out + pb) = four(4);
+                    }
+                    out += out_step;
+                }
+            }
+        }
+        pos = pos_next;
+        pos_next = pos_after;
+    }
+}
+
+// Backward.  Warps stride over the tokens and keep the weights' gradients in registers; at the end a CTA adds its warps' up, in
+// their order, and leaves the sums for rope_weights_kernel.
+template <int D, bool kPairs, typename T>
+__global__ void __launch_bounds__(kBackThreads, 2) rope_backward_kernel(const RopeArgs a)
+{
+    constexpr int kLanes = D / 8, kHeads = 32 / kLanes, kBatch = 2;
+    __shared__ float sums[kBackWarps * kHeads][2][D];
+    pdl_launch_next();
+    const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, l = lane % kLanes, mine = lane / kLanes;
+    const Pieces p = pieces_of<kPairs>(l, a.half);
+    Eight dw[2] = {};
+    pdl_wait();
+    for (int64_t token = (int64_t)blockIdx.x * kBackWarps + wid; token < a.tokens; token += (int64_t)gridDim.x * kBackWarps) {
         const int32_t pos = a.positions[token];
         const bool there = pos >= 0 && pos < a.max_positions;
         const int64_t b = token / a.seq, n = token - b * a.seq;
-        float c[4], s[4];
-        load_angles(a, p, there ? pos : 0, c, s);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) s[i] = -s[i];
+        Angles t = {};
+        bool looked_up = false;
 #pragma unroll
         for (int which = 0; which < 2; ++which) {
             const int H = which ? a.Hkv : a.Hq;
             const pa_strides &sx = which ? a.sk : a.sq, &sd = which ? a.sko : a.sqo;
-            const __nv_bfloat16 *x_row = (which ? a.k : a.q) + b * sx.batch + n * sx.seq;
-            const T *d_row = static_cast<const T *>(which ? a.d_k : a.d_q) + b * sd.batch + n * sd.seq;
-            __nv_bfloat16 *out = (which ? a.k_out : a.q_out) + token * H * D;
-            float w[8];
-            load_weights(which ? a.k_weight : a.q_weight, a.w_f32, p, w);
-            for (int h0 = 0; h0 < H; h0 += kBatch * kHeads) {
-                uint2 ra[kBatch], rb[kBatch];
-                float g[kBatch][8];
+            const __nv_bfloat16 *x = (which ? a.k : a.q) + b * sx.batch + n * sx.seq + mine * sx.head;
+            const T *d = static_cast<const T *>(which ? a.d_k : a.d_q) + b * sd.batch + n * sd.seq + mine * sd.head;
+            __nv_bfloat16 *out = (which ? a.k_out : a.q_out) + (token * H + mine) * D;
+            uint2 ra[kBatch], rb[kBatch];
+            uint4 da[kBatch], db[kBatch];
+            auto load = [&](int h) {
 #pragma unroll
                 for (int y = 0; y < kBatch; ++y) {
-                    const int h = h0 + y * kHeads + mine;
                     ra[y] = rb[y] = make_uint2(0u, 0u);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) g[y][i] = 0.f;
-                    if (h < H && there) {
-                        ra[y] = ld8(x_row + h * sx.head + p.a);
-                        rb[y] = ld8(x_row + h * sx.head + p.b);
-                        load_gradient(d_row + h * sd.head, p, g[y]);
+                    da[y] = db[y] = make_uint4(0u, 0u, 0u, 0u);
+                    if (there && h + y * kHeads + mine < H) {
+                        const __nv_bfloat16 *src = x + y * kHeads * sx.head;
+                        const T *grad = d + y * kHeads * sd.head;
+                        ra[y] = ld8(src + p.a);
+                        rb[y] = ld8(src + p.b);
+                        if constexpr (sizeof(T) == 4) {
+                            da[y] = *reinterpret_cast<const uint4 *>(grad + p.a);
+                            db[y] = *reinterpret_cast<const uint4 *>(grad + p.b);
+                        } else {
+                            const uint2 u = ld8(grad + p.a), v = ld8(grad + p.b);
+                            da[y] = make_uint4(u.x, u.y, 0u, 0u);
+                            db[y] = make_uint4(v.x, v.y, 0u, 0u);
+                        }
                     }
                 }
+                x += kBatch * kHeads * sx.head;
+                d += kBatch * kHeads * sd.head;
+            };
+            load(0);
+            const Eight w = load_weights<kPairs>(which ? a.k_weight : a.q_weight, a.w_f32, p);
+            if (!looked_up) {
+                t = load_angles(a, p, there ? pos : 0);
+                looked_up = true;
+            }
+            for (int h = 0; h < H; h += kBatch * kHeads) {
+                Eight v[kBatch], g[kBatch];
 #pragma unroll
                 for (int y = 0; y < kBatch; ++y) {
-                    const int h = h0 + y * kHeads + mine;
-                    float v[8];
-                    unpack4(ra[y], v);
-                    unpack4(rb[y], v + 4);
-                    if (p.rotated) rotate(g[y], c, s, a.interleaved);
-                    float sq = 0.f, along = 0.f;
+                    v[y] = from_bf16<kPairs>(ra[y], rb[y]);
+                    if constexpr (sizeof(T) == 4)
+                        g[y] = in_order<kPairs>(__uint_as_float(da[y].x), __uint_as_float(da[y].y), __uint_as_float(da[y].z),
+                                                __uint_as_float(da[y].w), __uint_as_float(db[y].x), __uint_as_float(db[y].y),
+                                                __uint_as_float(db[y].z), __uint_as_float(db[y].w));
+                    else
+                        g[y] = from_bf16<kPairs>(make_uint2(da[y].x, da[y].y), make_uint2(db[y].x, db[y].y));
+                }
+                if (h + kBatch * kHeads < H) load(h + kBatch * kHeads);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        sq = fmaf(v[i], v[i], sq);
-                        along = fmaf(g[y][i] * w[i], v[i], along);
+                for (int y = 0; y < kBatch; ++y) {
+                    const bool in = h + y * kHeads + mine < H;
+                    if (p.rotated) {  // back by the angle
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            const uint64_t f = g[y].v[i], s = g[y].v[2 + i];
+                            g[y].v[i] = fma_f32x2(f, t.c[i], mul_f32x2(s, t.s[i]));
+                            g[y].v[2 + i] = fma_f32x2(s, t.c[i], negative(mul_f32x2(f, t.s[i])));
+                        }
                     }
-                    sq = sum_lanes<kLanes>(sq);
-                    along = sum_lanes<kLanes>(along);
-                    // dx = r (h - x r^2 mean(h x)), h = g w
+                    // dx = r (h - x^ mean(h x^)), h = g w, x^ = x r;  dw = sum g x^
+                    Eight gw;
+                    uint64_t sq = 0, along = 0;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        gw.v[i] = mul_f32x2(g[y].v[i], w.v[i]);
+                        sq = fma_f32x2(v[y].v[i], v[y].v[i], sq);
+                        along = fma_f32x2(gw.v[i], v[y].v[i], along);
+                    }
+                    const float sum_sq = sum_lanes<kLanes>(sum_pairs(sq)), sum_along = sum_lanes<kLanes>(sum_pairs(along));
                     // (no head, no gradient, whatever eps is)
-                    const float r = h < H && there ? rsqrtf(sq * (1.0f / D) + a.eps) : 0.f, t = along * (1.0f / D) * r * r;
-                    float dx[8];
+                    const float r = in && there ? rsqrtf(sum_sq * (1.0f / D) + a.eps) : 0.f;
+                    const uint64_t r2 = both(r), mean = both(-sum_along * (1.0f / D) * r);
+                    Eight dx;
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        dx[i] = r * (g[y][i] * w[i] - v[i] * t);
-                        dw[which][i] = fmaf(g[y][i], v[i] * r, dw[which][i]);
+                    for (int i = 0; i < 4; ++i) {
+                        const uint64_t xn = mul_f32x2(v[y].v[i], r2);
+                        dw[which].v[i] = fma_f32x2(g[y].v[i], xn, dw[which].v[i]);
+                        dx.v[i] = mul_f32x2(r2, fma_f32x2(xn, mean, gw.v[i]));
                     }
-                    if (h < H) {
-                        *reinterpret_cast<uint2 *>(out + h * D + p.a) = pack4(dx);
-                        *reinterpret_cast<uint2 *>(out + h * D + p.b) = pack4(dx + 4);
-                    }
+                    if (in) write_bf16<kPairs>(dx, out + p.a, out + p.b);
+                    out += kHeads * D;
                 }
             }
         }
     }
     float(*row)[D] = sums[wid * kHeads + mine];
 #pragma unroll
-    for (int which = 0; which < 2; ++which)
+    for (int which = 0; which < 2; ++which) {
+        float x[8];
+        pieces<kPairs>(dw[which], x);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            row[which][p.a + i] = dw[which][i];
-            row[which][p.b + i] = dw[which][4 + i];
+            row[which][p.a + i] = x[i];
+            row[which][p.b + i] = x[4 + i];
         }
+    }
     __syncthreads();
-    for (int f = threadIdx.x; f < 2 * D; f += kRopeThreads) {
+    for (int f = threadIdx.x; f < 2 * D; f += kBackThreads) {
         float t = 0.f;
-        for (int y = 0; y < kRopeWarps * kHeads; ++y) t += sums[y][f / D][f % D];
+        for (int y = 0; y < kBackWarps * kHeads; ++y) t += sums[y][f / D][f % D];
         a.parts[(int64_t)blockIdx.x * 2 * D + f] = t;
     }
 }
@@ -303,8 +470,8 @@ static pa_status check_rope(const pa_rope_params *p)
     if (p->batch < 1 || p->n_q_heads < 1 || p->n_kv_heads < 1 || p->seq_len < 1 || p->max_positions < 1)
         return fail(PA_ERR_INVALID_ARG, "batch, head counts, seq_len and max_positions must be positive");
     if (p->head_dim != 64 && p->head_dim != 128) return fail(PA_ERR_SHAPE, "head_dim must be 64 or 128");
-    if (p->rotary_dim < 0 || p->rotary_dim > p->head_dim || p->rotary_dim % 8)
-        return fail(PA_ERR_SHAPE, "rotary_dim must be a multiple of 8 between 0 and head_dim");
+    if (p->rotary_dim < 0 || p->rotary_dim > p->head_dim || p->rotary_dim % 16)
+        return fail(PA_ERR_SHAPE, "rotary_dim must be a multiple of 16 between 0 and head_dim");
     if (!(p->eps >= 0.f) || isinf(p->eps)) return fail(PA_ERR_INVALID_ARG, "eps must be finite and >= 0");
     if (p->w_dtype != PA_BF16 && p->w_dtype != PA_F32) return fail(PA_ERR_INVALID_ARG, "bad w_dtype");
     if (p->n_q_heads > 65535 || p->n_kv_heads > 65535) return fail(PA_ERR_SHAPE, "head counts must be <= 65535");
@@ -358,19 +525,19 @@ static pa_status rope_args(const pa_rope_params *p, const void *q, const void *k
     a->Hkv = p->n_kv_heads;
     a->half = p->rotary_dim / 2;
     a->max_positions = p->max_positions;
-    a->interleaved = p->interleaved != 0;
     a->w_f32 = p->w_dtype == PA_F32;
     a->eps = p->eps;
     return PA_OK;
 }
 
-// CTAs of rope_backward_kernel, for the workspace and the launch alike.
-constexpr int64_t kRopeBackwardCtas = 148 * 4;
-static int64_t backward_ctas(const pa_rope_params *p)
+// CTAs of the kernels that stride over the tokens, a warp a token: two per SM (the workspace holds a part for each).
+constexpr int64_t kRopeCtas = 148 * 2;
+static int64_t token_ctas(const pa_rope_params *p)
 {
-    const int64_t need = ((int64_t)p->batch * p->seq_len + kRopeWarps - 1) / kRopeWarps;
-    return need < kRopeBackwardCtas ? need : kRopeBackwardCtas;
+    const int64_t need = ((int64_t)p->batch * p->seq_len + kBackWarps - 1) / kBackWarps;
+    return need < kRopeCtas ? need : kRopeCtas;
 }
+constexpr int64_t kRopeFewWarps = 148 * 64;  // warps that run all at once
 
 }  // namespace pa
 
@@ -386,17 +553,19 @@ extern "C" pa_status pa_qk_norm_rope(const pa_rope_params *p, const void *q, con
     if (pa_status s = rope_args(p, q, k, q_weight, k_weight, cos_sin, positions, q_out, k_out, q_out, k_out, &a)) return s;
     a.q_out = static_cast<__nv_bfloat16 *>(q_out);
     a.k_out = static_cast<__nv_bfloat16 *>(k_out);
-    const int heads = p->n_q_heads + p->n_kv_heads, at_once = 256 / p->head_dim;
-    // Few tokens: one batch of heads a warp, so that the call is as short as a warp's chain of loads.
-    const bool few = a.tokens * heads <= 148 * 64 * at_once;
-    a.heads_per_chunk = few ? at_once : heads;
-    a.chunks = (heads + a.heads_per_chunk - 1) / a.heads_per_chunk;
-    const int64_t ctas = (a.tokens * a.chunks + kRopeWarps - 1) / kRopeWarps;
-    if (ctas > INT32_MAX) return fail(PA_ERR_SHAPE, "too many tokens");
+    const int at_once = 256 / p->head_dim;
+    a.chunks = (p->n_q_heads + at_once - 1) / at_once + (p->n_kv_heads + at_once - 1) / at_once;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    auto launch = [&](auto kernel) { return launch_pdl(kernel, dim3((unsigned)ctas), kRopeThreads, 0, st, a); };
-    PA_CUDA_OK(p->head_dim == 128 ? (few ? launch(rope_kernel<128, 1>) : launch(rope_kernel<128, 4>))
-                                  : (few ? launch(rope_kernel<64, 1>) : launch(rope_kernel<64, 4>)));
+    static void (*const few[2][2])(const RopeArgs) = {{rope_few_kernel<64, false>, rope_few_kernel<64, true>},
+                                                      {rope_few_kernel<128, false>, rope_few_kernel<128, true>}};
+    static void (*const many[2][2])(const RopeArgs) = {{rope_kernel<64, false>, rope_kernel<64, true>},
+                                                       {rope_kernel<128, false>, rope_kernel<128, true>}};
+    const int64_t warps = a.tokens * a.chunks;
+    if (warps <= kRopeFewWarps)
+        PA_CUDA_OK(launch_pdl(few[p->head_dim == 128][p->interleaved != 0], dim3((unsigned)((warps + kRopeWarps - 1) / kRopeWarps)),
+                              kRopeThreads, 0, st, a));
+    else
+        PA_CUDA_OK(launch_pdl(many[p->head_dim == 128][p->interleaved != 0], dim3((unsigned)token_ctas(p)), kBackThreads, 0, st, a));
     return PA_OK;
 }
 
@@ -404,7 +573,7 @@ extern "C" size_t pa_qk_norm_rope_backward_workspace_bytes(const pa_rope_params 
 {
     using namespace pa;
     if (check_rope(p) != PA_OK) return 0;
-    return (size_t)backward_ctas(p) * 2 * p->head_dim * sizeof(float);
+    return (size_t)token_ctas(p) * 2 * p->head_dim * sizeof(float);
 }
 
 extern "C" pa_status pa_qk_norm_rope_backward(const pa_rope_params *p, const void *q, const void *k, const void *q_weight,
@@ -430,12 +599,15 @@ extern "C" pa_status pa_qk_norm_rope_backward(const pa_rope_params *p, const voi
     a.d_q = d_q_out;
     a.d_k = d_k_out;
     a.parts = static_cast<float *>(workspace);
-    const int64_t ctas = backward_ctas(p);
+    const int64_t ctas = token_ctas(p);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    auto launch = [&](auto kernel) { return launch_pdl(kernel, dim3((unsigned)ctas), kRopeThreads, 0, st, a); };
-    const bool f32 = d_dtype == PA_F32;
-    PA_CUDA_OK(p->head_dim == 128 ? (f32 ? launch(rope_backward_kernel<128, float>) : launch(rope_backward_kernel<128, __nv_bfloat16>))
-                                  : (f32 ? launch(rope_backward_kernel<64, float>) : launch(rope_backward_kernel<64, __nv_bfloat16>)));
+    using bf16 = __nv_bfloat16;
+    static void (*const kernels[2][2][2])(const RopeArgs) = {{{rope_backward_kernel<64, false, bf16>, rope_backward_kernel<64, false, float>},
+                                                              {rope_backward_kernel<64, true, bf16>, rope_backward_kernel<64, true, float>}},
+                                                             {{rope_backward_kernel<128, false, bf16>, rope_backward_kernel<128, false, float>},
+                                                              {rope_backward_kernel<128, true, bf16>, rope_backward_kernel<128, true, float>}}};
+    auto launch = [&](auto kernel) { return launch_pdl(kernel, dim3((unsigned)ctas), kBackThreads, 0, st, a); };
+    PA_CUDA_OK(launch(kernels[p->head_dim == 128][p->interleaved != 0][d_dtype == PA_F32]));
     PA_CUDA_OK(launch_pdl(rope_weights_kernel, dim3((unsigned)(2 * p->head_dim / 32)), 1024, 0, st,
                           static_cast<const float *>(a.parts), (int)ctas, (int)p->head_dim, dq_weight, dk_weight));
     return PA_OK;

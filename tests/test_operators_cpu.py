@@ -70,7 +70,7 @@ def test_rope_refusals(b):
         for bad in (dict(batch=0), dict(n_q_heads=0), dict(n_kv_heads=0), dict(seq_len=0), dict(max_positions=0), dict(eps=-1.0),
                     dict(eps=float("nan")), dict(eps=float("inf")), dict(w_dtype=7)):
             assert call(_changed(good, **bad)) == "PA_ERR_INVALID_ARG", bad
-        for bad in (dict(head_dim=96), dict(rotary_dim=132), dict(rotary_dim=-8), dict(rotary_dim=20), dict(n_q_heads=70000),
+        for bad in (dict(head_dim=96), dict(rotary_dim=132), dict(rotary_dim=-8), dict(rotary_dim=24), dict(n_q_heads=70000),
                     dict(seq_len=1 << 40), dict(q=b.pa_strides(0, -8, 128))):
             assert call(_changed(good, **bad)) == "PA_ERR_SHAPE", bad
         assert call(_changed(good, k=b.pa_strides(0, 516, 128))) == "PA_ERR_ALIGNMENT"
