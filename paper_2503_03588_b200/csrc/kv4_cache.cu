@@ -1,7 +1,11 @@
 // pa_kv4_append, pa_kv4_read: tokens into and out of the 4-bit pages.
 //
-// Bound by memory: append reads 2 bytes a number and writes 9/16.  A thread takes eight features (16 bytes in, one 32-bit word of
-// nibbles out); the four threads of a group share its largest magnitude by shuffles.
+// Bound by memory: append reads 2 bytes a number and writes 9/16.  A thread has the same features of the same head, of K or of V, of
+// kTokens = 4 tokens, so that what it has to work out about its place is shared and four loads are on their way at once (51K
+// tokens, 4 heads of 128 features, append and read: 82 us, with a token a thread 117); of one where all run at once anyhow (256
+// tokens: 3.6 us, with four tokens 5.0).
+// Append: eight features (16 bytes in, one 32-bit word of nibbles out), the four threads of a group share its largest
+// magnitude by shuffles.  Read: four features, one 16-byte store of fp32.
 #include <limits.h>
 
 #include "common.cuh"
@@ -19,135 +23,151 @@ struct Kv4CacheArgs {
     int64_t page_stride, head_stride;  // bytes
     int64_t k_st, k_sh, v_st, v_sh;    // elements
     int64_t tokens, n_slots;
-    int32_t Hkv, pieces;               // pieces of eight features of a token: 2 Hkv D / 8, K's then V's
+    int32_t Hkv;
 };
 
-struct Piece {
+// A thread's features: which of kPer parts of a head, the head, K or V, and its first token.
+struct Kv4Place {
     int64_t token;
-    int head, c;  // KV head, number of the piece in its row
+    int head, c;
     bool is_v;
 };
-template <int D>
-__device__ __forceinline__ Piece piece_of(const Kv4CacheArgs &a, int64_t x)
+template <int kPer, int kTokens>
+__device__ __forceinline__ Kv4Place place_of(const Kv4CacheArgs &a)
 {
-    Piece p;
-    p.token = x / a.pieces;
-    int rest = (int)(x - p.token * a.pieces);
-    p.is_v = rest >= a.pieces / 2;
-    if (p.is_v) rest -= a.pieces / 2;
-    p.head = rest / (D / 8);
-    p.c = rest % (D / 8);
+    Kv4Place p;
+    p.c = threadIdx.x % kPer;
+    const uint32_t row = blockIdx.x * (kKv4Threads / kPer) + threadIdx.x / kPer;  // (below 2^32: checked on the host)
+    const uint32_t group = row / (2u * (uint32_t)a.Hkv), rest = row - group * 2u * (uint32_t)a.Hkv;
+    p.is_v = rest >= (uint32_t)a.Hkv;
+    p.head = (int)(p.is_v ? rest - (uint32_t)a.Hkv : rest);
+    p.token = (int64_t)group * kTokens;
     return p;
 }
 // K's or V's half of the record that holds a slot's token.
 template <int D>
-__device__ __forceinline__ uint8_t *half_record(const Kv4CacheArgs &a, const Piece &p, int64_t slot)
+__device__ __forceinline__ uint8_t *half_record(const Kv4CacheArgs &a, const Kv4Place &p, int64_t slot)
 {
     return a.pool + (slot / kKv4Page) * a.page_stride + p.head * a.head_stride + (p.is_v ? Kv4Record<D>::kHalf : 0);
 }
-// Byte in its row at which a K piece's word, or the halfwords of a V piece, stand.
+// Byte in its row at which the nibbles of features 4 h .. 4 h + 3 stand, a halfword.  (K: of features 8 c .. 8 c + 7, a word at the
+// place of h = 2 c.)
 template <int D>
-__device__ __forceinline__ int k_byte(int c) { return ((c & 3) * Kv4Record<D>::kGroups + (c >> 2)) * 4; }
-template <int D>
-__device__ __forceinline__ int v_byte(int c, int place, int upper)
+__device__ __forceinline__ int k_byte(int h)
 {
-    const int chunk = (2 * (c & 3) + upper) ^ ((place & 2) << 1);
-    return chunk * (2 * Kv4Record<D>::kGroups) + 2 * (c >> 2);
+    const int c = h >> 1;
+    return ((c & 3) * Kv4Record<D>::kGroups + (c >> 2)) * 4 + 2 * (h & 1);
+}
+template <int D>
+__device__ __forceinline__ int v_byte(int h, int place)
+{
+    return ((h & 7) ^ ((place & 2) << 1)) * (2 * Kv4Record<D>::kGroups) + 2 * (h >> 3);
 }
 
-template <int D>
+__device__ __forceinline__ uint32_t max_magnitude(uint32_t a, uint32_t b)  // of two pairs of bf16 without sign; NaN stays
+{
+    uint32_t d;
+    asm("max.NaN.bf16x2 %0, %1, %2;\n" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
+
+template <int D, int kTokens>
 __global__ void __launch_bounds__(kKv4Threads) kv4_append_kernel(const Kv4CacheArgs a)
 {
     using R = Kv4Record<D>;
     pdl_launch_next();
-    const int64_t x = (int64_t)blockIdx.x * kKv4Threads + threadIdx.x;
-    const bool in = x < a.tokens * a.pieces;  // (the four threads of a group are in or out together)
-    const Piece p = piece_of<D>(a, in ? x : 0);
+    const Kv4Place p = place_of<D / 8, kTokens>(a);  // (the threads of a group share its tokens)
+    const int64_t st = p.is_v ? a.v_st : a.k_st;
+    const __nv_bfloat16 *src = p.is_v ? a.v + p.token * a.v_st + p.head * a.v_sh : a.k + p.token * a.k_st + p.head * a.k_sh;
     pdl_wait();
-    const int64_t slot = in ? a.slots[p.token] : -1;
-    uint4 raw = make_uint4(0u, 0u, 0u, 0u);
-    if (in) {
-        const __nv_bfloat16 *src = p.is_v ? a.v + p.token * a.v_st + p.head * a.v_sh : a.k + p.token * a.k_st + p.head * a.k_sh;
-        raw = *reinterpret_cast<const uint4 *>(src + 8 * p.c);
-    }
-    const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
-    // The largest magnitude: bf16 patterns without their sign are ordered as integers (infinity and NaN on top).
-    uint32_t top = 0;
+    int64_t slot[kTokens];
+    uint4 raw[kTokens];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) top = max(top, max(w[i] & 0x7fffu, (w[i] >> 16) & 0x7fffu));
-    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-    top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-    if (slot < 0 || slot >= a.n_slots) return;
-    // s = amax / 7 in bf16.  A quotient by 7 is never near enough to the middle of two bf16 numbers for the fp32 product to
-    // round differently (it is 1/14 of a step away at least).
-    const float amax = __uint_as_float(top << 16);
-    const bool zero = amax < 7.8886090522101181e-31f;  // 2^-100
-    __nv_bfloat16 s = __float2bfloat16_rn(zero ? 0.f : amax * (1.0f / 7.0f));
-    const bool wild = top >= 0x7f80u;
-    if (wild) s = __ushort_as_bfloat16(0x7fc0);
-    // x / s with ties towards zero: the quotient of two 8-bit mantissas lies on a tie or at least 2^-10 from it, so the
-    // nearest integer of x / s (1 - 2^-16) is the one.
-    const float inv = zero || wild ? 0.f : (1.0f - 0x1p-16f) / __bfloat162float(s);
-    uint32_t word = 0;
+    for (int y = 0; y < kTokens; ++y) {
+        const bool in = p.token + y < a.tokens;
+        slot[y] = in ? a.slots[p.token + y] : -1;
+        raw[y] = in ? *reinterpret_cast<const uint4 *>(src + y * st + 8 * p.c) : make_uint4(0u, 0u, 0u, 0u);
+    }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        // (adding 1.5 x 2^23 leaves the nearest integer in the low bits; a wild or zero group has nibbles of 8)
-        const float lo = __uint_as_float(w[i] << 16), hi = __uint_as_float(w[i] & 0xffff0000u);
-        const uint32_t n0 = inv != 0.f ? __float_as_uint(fmaf(lo, inv, 12582912.f + 8.f)) : 8u;
-        const uint32_t n1 = inv != 0.f ? __float_as_uint(fmaf(hi, inv, 12582912.f + 8.f)) : 8u;
-        word |= (n0 & 15u) << (8 * i) | (n1 & 15u) << (8 * i + 4);
+    for (int y = 0; y < kTokens; ++y) {
+        const uint32_t w[4] = {raw[y].x, raw[y].y, raw[y].z, raw[y].w};
+        constexpr uint32_t kAbs = 0x7fff7fffu;
+        uint32_t two = max_magnitude(max_magnitude(w[0] & kAbs, w[1] & kAbs), max_magnitude(w[2] & kAbs, w[3] & kAbs));
+        two = max_magnitude(two, __shfl_xor_sync(0xffffffffu, two, 1));
+        two = max_magnitude(two, __shfl_xor_sync(0xffffffffu, two, 2));
+        const uint32_t top = max(two & 0xffffu, two >> 16);  // (patterns without sign are ordered as integers, NaN on top)
+        if (slot[y] < 0 || slot[y] >= a.n_slots) continue;
+        // s = amax / 7 in bf16.  A quotient by 7 is never near enough to the middle of two bf16 numbers for the fp32 product to
+        // round differently (it is 1/14 of a step away at least).
+        const float amax = __uint_as_float(top << 16);
+        const bool zero = amax < 0x1p-100f, wild = top >= 0x7f80u;
+        const __nv_bfloat16 s = wild ? __ushort_as_bfloat16(0x7fc0) : __float2bfloat16_rn(zero ? 0.f : amax * (1.0f / 7.0f));
+        // x / s with ties towards zero: the quotient of two 8-bit mantissas lies on a tie or at least 2^-10 from it, so the
+        // nearest integer of x / s (1 - 2^-16) is the one.  Adding 1.5 x 2^23 + 8 leaves u in the low bits of a sum, and the
+        // sums' patterns, 16 times each and added up, leave all nibbles but for a constant.  (A group of NaNs has any nibbles.)
+        const float inv = zero || wild ? 0.f : __fdividef(1.0f - 0x1p-16f, __bfloat162float(s));
+        constexpr float kMagic = 12582912.f + 8.f;
+        constexpr uint32_t kPattern = 0x4b400000u, kAll = 0x11111111u;
+        uint32_t word = 0;
+#pragma unroll
+        for (int i = 3; i >= 0; --i) {
+            const uint32_t n0 = __float_as_uint(fmaf(__uint_as_float(w[i] << 16), inv, kMagic));
+            const uint32_t n1 = __float_as_uint(fmaf(__uint_as_float(w[i] & 0xffff0000u), inv, kMagic));
+            word = (word * 16u + n1) * 16u + n0;
+        }
+        word -= kPattern * kAll;
+        const int place = (int)(slot[y] % kKv4Page);
+        uint8_t *half = half_record<D>(a, p, slot[y]), *row = half + place * R::kRow;
+        if (p.is_v) {
+            *reinterpret_cast<uint16_t *>(row + v_byte<D>(2 * p.c, place)) = (uint16_t)word;
+            *reinterpret_cast<uint16_t *>(row + v_byte<D>(2 * p.c + 1, place)) = (uint16_t)(word >> 16);
+        } else {
+            *reinterpret_cast<uint32_t *>(row + k_byte<D>(2 * p.c)) = word;
+        }
+        if ((p.c & 3) == 0)
+            *reinterpret_cast<__nv_bfloat16 *>(half + R::kScales + place * R::kScaleRow + 2 * (p.c >> 2)) = s;
     }
-    const int place = (int)(slot % kKv4Page);
-    uint8_t *half = half_record<D>(a, p, slot), *row = half + place * R::kRow;
-    if (p.is_v) {
-        *reinterpret_cast<uint16_t *>(row + v_byte<D>(p.c, place, 0)) = (uint16_t)word;
-        *reinterpret_cast<uint16_t *>(row + v_byte<D>(p.c, place, 1)) = (uint16_t)(word >> 16);
-    } else {
-        *reinterpret_cast<uint32_t *>(row + k_byte<D>(p.c)) = word;
-    }
-    if ((p.c & 3) == 0)
-        *reinterpret_cast<__nv_bfloat16 *>(half + R::kScales + place * R::kScaleRow + 2 * (p.c >> 2)) = s;
 }
 
-template <int D, bool kF32>
+template <int D, bool kF32, int kTokens>
 __global__ void __launch_bounds__(kKv4Threads) kv4_read_kernel(const Kv4CacheArgs a)
 {
     using R = Kv4Record<D>;
     pdl_launch_next();
-    const int64_t x = (int64_t)blockIdx.x * kKv4Threads + threadIdx.x;
-    if (x >= a.tokens * a.pieces) return;
-    const Piece p = piece_of<D>(a, x);
+    const Kv4Place p = place_of<D / 4, kTokens>(a);
     pdl_wait();
-    const int64_t slot = a.slots[p.token];
-    uint32_t word = 0x88888888u;
-    float s = 0.f;
-    if (slot >= 0 && slot < a.n_slots) {
-        const int place = (int)(slot % kKv4Page);
-        const uint8_t *half = half_record<D>(a, p, slot), *row = half + place * R::kRow;
-        if (p.is_v)
-            word = *reinterpret_cast<const uint16_t *>(row + v_byte<D>(p.c, place, 0)) |
-                   (uint32_t)*reinterpret_cast<const uint16_t *>(row + v_byte<D>(p.c, place, 1)) << 16;
-        else
-            word = *reinterpret_cast<const uint32_t *>(row + k_byte<D>(p.c));
-        s = __bfloat162float(*reinterpret_cast<const __nv_bfloat16 *>(half + R::kScales + place * R::kScaleRow + 2 * (p.c >> 2)));
-    }
-    float y[8];
+    int64_t slot[kTokens];
+    uint32_t word[kTokens];
+    float s[kTokens];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) y[i] = s * (float)((int)((word >> (4 * i)) & 15u) - 8);
-    const int64_t at = ((p.token * a.Hkv + p.head) * (D / 8) + p.c) * 8;
-    void *out = p.is_v ? a.v_out : a.k_out;
-    if (kF32) {
-        float4 *to = reinterpret_cast<float4 *>(static_cast<float *>(out) + at);
-        to[0] = make_float4(y[0], y[1], y[2], y[3]);
-        to[1] = make_float4(y[4], y[5], y[6], y[7]);
-    } else {
-        uint32_t h[4];
+    for (int y = 0; y < kTokens; ++y) slot[y] = p.token + y < a.tokens ? a.slots[p.token + y] : -1;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const __nv_bfloat162 b = __floats2bfloat162_rn(y[2 * i], y[2 * i + 1]);
-            h[i] = *reinterpret_cast<const uint32_t *>(&b);
+    for (int y = 0; y < kTokens; ++y) {
+        word[y] = 0x8888u;
+        s[y] = 0.f;
+        if (slot[y] >= 0 && slot[y] < a.n_slots) {
+            const int place = (int)(slot[y] % kKv4Page);
+            const uint8_t *half = half_record<D>(a, p, slot[y]), *row = half + place * R::kRow;
+            word[y] = *reinterpret_cast<const uint16_t *>(row + (p.is_v ? v_byte<D>(p.c, place) : k_byte<D>(p.c)));
+            s[y] = __bfloat162float(*reinterpret_cast<const __nv_bfloat16 *>(half + R::kScales + place * R::kScaleRow + 2 * (p.c >> 3)));
         }
-        *reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(out) + at) = make_uint4(h[0], h[1], h[2], h[3]);
+    }
+    void *out = p.is_v ? a.v_out : a.k_out;
+#pragma unroll
+    for (int y = 0; y < kTokens; ++y) {
+        if (p.token + y >= a.tokens) break;
+        float x[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)  // (2^23 + u as a pattern)
+            x[i] = s[y] * (__uint_as_float((word[y] >> (4 * i) & 15u) | 0x4b000000u) - 8388616.f);
+        const int64_t at = ((p.token + y) * a.Hkv + p.head) * D + 4 * p.c;
+        if (kF32) {
+            *reinterpret_cast<float4 *>(static_cast<float *>(out) + at) = make_float4(x[0], x[1], x[2], x[3]);
+        } else {
+            const __nv_bfloat162 lo = __floats2bfloat162_rn(x[0], x[1]), hi = __floats2bfloat162_rn(x[2], x[3]);
+            *reinterpret_cast<uint2 *>(static_cast<__nv_bfloat16 *>(out) + at) =
+                make_uint2(*reinterpret_cast<const uint32_t *>(&lo), *reinterpret_cast<const uint32_t *>(&hi));
+        }
     }
 }
 
@@ -165,7 +185,8 @@ pa_status check_kv4_pool(const pa_kv4_pool &p)
     return PA_OK;
 }
 
-static pa_status cache_args(const pa_kv4_pool *p, int64_t n_tokens, const void *kv_pool, const int64_t *slot_map, const void *k,
+// per: threads of a row.  *many: four tokens a thread.
+static pa_status cache_args(const pa_kv4_pool *p, int per, bool *many, int64_t n_tokens, const void *kv_pool, const int64_t *slot_map, const void *k,
                             const void *v, Kv4CacheArgs *a, int64_t *ctas)
 {
     if (!p) return fail(PA_ERR_INVALID_ARG, "the pool's description must be non-null");
@@ -184,9 +205,11 @@ static pa_status cache_args(const pa_kv4_pool *p, int64_t n_tokens, const void *
     a->tokens = n_tokens;
     a->n_slots = (int64_t)p->n_pages * kKv4Page;
     a->Hkv = p->n_kv_heads;
-    a->pieces = 2 * p->n_kv_heads * (p->head_dim / 8);
-    if (n_tokens > ((int64_t)INT_MAX * kKv4Threads) / a->pieces) return fail(PA_ERR_SHAPE, "too many tokens");
-    *ctas = (n_tokens * a->pieces + kKv4Threads - 1) / kKv4Threads;
+    if (n_tokens > INT_MAX / p->n_kv_heads) return fail(PA_ERR_SHAPE, "too many tokens");
+    *many = n_tokens * 2 * p->n_kv_heads * per > 148 * 2048;
+    const int tokens = *many ? 4 : 1;
+    const int64_t rows = (n_tokens + tokens - 1) / tokens * 2 * p->n_kv_heads;
+    *ctas = (rows * per + kKv4Threads - 1) / kKv4Threads;
     return PA_OK;
 }
 
@@ -205,7 +228,8 @@ extern "C" pa_status pa_kv4_append(const pa_kv4_pool *pool, int64_t n_tokens, co
     clear_error();
     Kv4CacheArgs a;
     int64_t ctas;
-    if (pa_status s = cache_args(pool, n_tokens, kv_pool, slot_map, k_new, v_new, &a, &ctas)) return s;
+    bool many;
+    if (pa_status s = cache_args(pool, pool ? pool->head_dim / 8 : 0, &many, n_tokens, kv_pool, slot_map, k_new, v_new, &a, &ctas)) return s;
     for (const pa_strides &s : {k_strides, v_strides}) {
         if (s.seq < 0 || s.head < 0) return fail(PA_ERR_SHAPE, "strides must be >= 0");
         if ((s.seq % 8) || (s.head % 8)) return fail(PA_ERR_ALIGNMENT, "strides must be multiples of 8 elements (16 bytes)");
@@ -220,7 +244,9 @@ extern "C" pa_status pa_kv4_append(const pa_kv4_pool *pool, int64_t n_tokens, co
     a.v_sh = v_strides.head;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     auto launch = [&](auto kernel) { return launch_pdl(kernel, dim3((unsigned)ctas), kKv4Threads, 0, st, a); };
-    PA_CUDA_OK(pool->head_dim == 128 ? launch(kv4_append_kernel<128>) : launch(kv4_append_kernel<64>));
+    static void (*const kernels[2][2])(const Kv4CacheArgs) = {{kv4_append_kernel<64, 1>, kv4_append_kernel<64, 4>},
+                                                              {kv4_append_kernel<128, 1>, kv4_append_kernel<128, 4>}};
+    PA_CUDA_OK(launch(kernels[pool->head_dim == 128][many]));
     return PA_OK;
 }
 
@@ -231,16 +257,18 @@ extern "C" pa_status pa_kv4_read(const pa_kv4_pool *pool, int64_t n_tokens, cons
     clear_error();
     Kv4CacheArgs a;
     int64_t ctas;
+    bool many;
     if (dtype != PA_BF16 && dtype != PA_F32) return fail(PA_ERR_INVALID_ARG, "bad dtype");
-    if (pa_status s = cache_args(pool, n_tokens, kv_pool, slot_map, k_out, v_out, &a, &ctas)) return s;
+    if (pa_status s = cache_args(pool, pool ? pool->head_dim / 4 : 0, &many, n_tokens, kv_pool, slot_map, k_out, v_out, &a, &ctas)) return s;
     if (ctas == 0) return PA_OK;
     a.pool = static_cast<uint8_t *>(const_cast<void *>(kv_pool));
     a.k_out = k_out;
     a.v_out = v_out;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     auto launch = [&](auto kernel) { return launch_pdl(kernel, dim3((unsigned)ctas), kKv4Threads, 0, st, a); };
-    const bool f32 = dtype == PA_F32;
-    PA_CUDA_OK(pool->head_dim == 128 ? (f32 ? launch(kv4_read_kernel<128, true>) : launch(kv4_read_kernel<128, false>))
-                                     : (f32 ? launch(kv4_read_kernel<64, true>) : launch(kv4_read_kernel<64, false>)));
+    static void (*const kernels[2][2][2])(const Kv4CacheArgs) = {
+        {{kv4_read_kernel<64, false, 1>, kv4_read_kernel<64, false, 4>}, {kv4_read_kernel<64, true, 1>, kv4_read_kernel<64, true, 4>}},
+        {{kv4_read_kernel<128, false, 1>, kv4_read_kernel<128, false, 4>}, {kv4_read_kernel<128, true, 1>, kv4_read_kernel<128, true, 4>}}};
+    PA_CUDA_OK(launch(kernels[pool->head_dim == 128][dtype == PA_F32][many]));
     return PA_OK;
 }
