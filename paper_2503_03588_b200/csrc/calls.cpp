@@ -7,6 +7,7 @@
 // set_error(status, message); broken preconditions raise AssertionError as the Python asserts did.
 #include <Python.h>
 
+#include <ATen/core/Tensor.h>
 #include <ATen/ops/empty.h>
 #include <c10/core/DefaultDtype.h>
 #include <c10/cuda/CUDAFunctions.h>
@@ -341,9 +342,49 @@ PyObject *build_layout(PyObject *const *x)
 template <typename... T>
 void on_current_device(const T &...tensors)
 {
-    for (const at::Tensor *t : {&tensors...})
-        expect(t->is_cuda() && t->get_device() == c10::cuda::current_device(), "expected tensors on the current CUDA device");
+    bool on = true;
+    for (const at::Tensor *t : {&tensors...}) on = on && t->is_cuda();
+    const int device = on ? c10::cuda::current_device() : 0;
+    for (const at::Tensor *t : {&tensors...}) on = on && t->get_device() == device;
+    expect(on, "expected tensors on the current CUDA device");
 }
+
+// The outputs that a call's caller has not given.  Small ones share one allocation: a call that takes the GPU 2 us spent 7 us of
+// host time on six of them.
+class Fresh {
+    struct One {
+        at::IntArrayRef size;
+        at::ScalarType type;
+        int64_t at, bytes;
+    };
+    const at::Tensor &like;
+    at::Tensor base;
+    int64_t total = 0;
+    c10::SmallVector<One, 8> list;
+
+public:
+    explicit Fresh(const at::Tensor &t) : like(t) {}
+    // An output that will be needed if `given` is None.  (`size` has to outlive this.)
+    void add(PyObject *given, at::IntArrayRef size, at::ScalarType type)
+    {
+        int64_t n = given == Py_None ? (int64_t)c10::elementSize(type) : 0;
+        for (const int64_t x : size) n *= x;
+        list.push_back({size, type, total, n});
+        total += (n + 255) / 256 * 256;
+    }
+    Out operator()(size_t i, PyObject *given)
+    {
+        const One &o = list[i];
+        return Out(given, [&]() -> at::Tensor {
+            if (total > (1 << 20)) return make(like, o.size, o.type);
+            if (!base.defined()) base = make(like, {total}, at::kByte);
+            at::Tensor t = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(base.storage()), base.key_set(), c10::scalarTypeToTypeMeta(o.type));
+            t.unsafeGetTensorImpl()->set_sizes_contiguous(o.size);
+            t.unsafeGetTensorImpl()->set_storage_offset(o.at / (int64_t)c10::elementSize(o.type));
+            return t;
+        });
+    }
+};
 bool is_bf16(const at::Tensor &t) { return t.scalar_type() == at::kBFloat16; }
 bool is_f32(const at::Tensor &t) { return t.scalar_type() == at::kFloat; }
 bool plain(const at::Tensor &t, at::ScalarType type, at::IntArrayRef size)
@@ -365,14 +406,18 @@ PyObject *build_block_tables(PyObject *const *x)
     expect(table.dim() == 2 && plain(table, at::kInt, {batch, table.size(1)}), "expected a contiguous int32 block table [batch, max_blocks]");
     expect(table.size(1) <= INT32_MAX && pages.numel() <= INT32_MAX && batch <= INT32_MAX && max_tokens >= 0, "too large or negative a size");
     on_current_device(fresh, cached, pages, count, table);
-    const Out cu(x[7], [&] { return make(fresh, {batch + 1}, at::kInt); });
-    const Out slots(x[8], [&] { return make(fresh, {max_tokens}, at::kLong); });
-    const Out positions(x[9], [&] { return make(fresh, {max_tokens}, at::kInt); });
-    const Out lens(x[10], [&] { return make(fresh, {batch}, at::kInt); });
-    const Out left(x[11], [&] { return make(fresh, {1}, at::kInt); });
     const pa_table_params p = {(int32_t)batch, block, (int32_t)table.size(1), n_pages, max_tokens,
                                (int32_t)pages.numel()};
-    const Out ws(x[12], [&] { return make_bytes(fresh, pa_build_block_tables_workspace_bytes(&p)); });
+    const int64_t some = batch + 1, tokens = max_tokens, one = 1, bytes = (int64_t)pa_build_block_tables_workspace_bytes(&p) + 16;
+    Fresh outs(fresh);
+    outs.add(x[7], some, at::kInt);
+    outs.add(x[8], tokens, at::kLong);
+    outs.add(x[9], tokens, at::kInt);
+    outs.add(x[10], batch, at::kInt);
+    outs.add(x[11], one, at::kInt);
+    outs.add(x[12], bytes, at::kByte);
+    const Out cu = outs(0, x[7]), slots = outs(1, x[8]), positions = outs(2, x[9]), lens = outs(3, x[10]), left = outs(4, x[11]),
+              ws = outs(5, x[12]);
     expect(plain(cu.t, at::kInt, {batch + 1}) && plain(slots.t, at::kLong, {max_tokens}) && plain(positions.t, at::kInt, {max_tokens}) &&
                plain(lens.t, at::kInt, {batch}) && plain(left.t, at::kInt, {1}),
            "expected contiguous int32 cu_seqlens [batch + 1], positions [max_tokens], lens_out [batch], free_left [1], int64 slot_map");
@@ -427,8 +472,10 @@ PyObject *qk_norm_rope(PyObject *const *x)
 {
     const at::Tensor &q = tensor(x[0]), &k = tensor(x[1]), &wq = tensor(x[2]), &wk = tensor(x[3]), &cos_sin = tensor(x[4]),
                      &positions = tensor(x[5]);
-    const Out q_out(x[6], [&] { return make(q, q.sizes(), at::kBFloat16); });
-    const Out k_out(x[7], [&] { return make(k, k.sizes(), at::kBFloat16); });
+    Fresh outs(q);
+    outs.add(x[6], q.sizes(), at::kBFloat16);
+    outs.add(x[7], k.sizes(), at::kBFloat16);
+    const Out q_out = outs(0, x[6]), k_out = outs(1, x[7]);
     expect(is_bf16(q_out.t) && is_bf16(k_out.t), "q_out and k_out are bfloat16");
     const pa_rope_params p = rope_params(q, k, wq, wk, cos_sin, positions, q_out.t, k_out.t, number(x[8]), truth(x[9]));
     run([&] {
@@ -446,11 +493,14 @@ PyObject *qk_norm_rope_backward(PyObject *const *x)
     expect(d_q.scalar_type() == d_k.scalar_type() && (is_bf16(d_q) || is_f32(d_q)),
            "the gradients of the outputs are both bfloat16 or both float32");
     const pa_rope_params p = rope_params(q, k, wq, wk, cos_sin, positions, d_q, d_k, number(x[13]), truth(x[14]));
-    const Out dq(x[8], [&] { return make(q, q.sizes(), at::kBFloat16); });
-    const Out dk(x[9], [&] { return make(k, k.sizes(), at::kBFloat16); });
-    const Out dwq(x[10], [&] { return make(q, {q.size(-1)}, at::kFloat); });
-    const Out dwk(x[11], [&] { return make(q, {q.size(-1)}, at::kFloat); });
-    const Out ws(x[12], [&] { return make_bytes(q, pa_qk_norm_rope_backward_workspace_bytes(&p)); });
+    const int64_t d = q.size(-1), bytes = (int64_t)pa_qk_norm_rope_backward_workspace_bytes(&p) + 16;
+    Fresh outs(q);
+    outs.add(x[8], q.sizes(), at::kBFloat16);
+    outs.add(x[9], k.sizes(), at::kBFloat16);
+    outs.add(x[10], d, at::kFloat);
+    outs.add(x[11], d, at::kFloat);
+    outs.add(x[12], bytes, at::kByte);
+    const Out dq = outs(0, x[8]), dk = outs(1, x[9]), dwq = outs(2, x[10]), dwk = outs(3, x[11]), ws = outs(4, x[12]);
     expect(plain(dq.t, at::kBFloat16, q.sizes()) && plain(dk.t, at::kBFloat16, k.sizes()) && plain(dwq.t, at::kFloat, {q.size(-1)}) &&
                plain(dwk.t, at::kFloat, {q.size(-1)}),
            "dq and dk are contiguous bfloat16, the weights' gradients float32 [head_dim]");
@@ -497,8 +547,11 @@ PyObject *kv4_read(PyObject *const *x)
     const pa_kv4_pool p = kv4_pool(pool, integer(x[2]));
     expect(plain(slots, at::kLong, {slots.numel()}), "slot_map is contiguous int64 [tokens]");
     const int64_t size[3] = {slots.numel(), p.n_kv_heads, p.head_dim};
-    const Out k(x[3], [&] { return make(pool, size, dtype(x[5])); });
-    const Out v(x[4], [&] { return make(pool, size, dtype(x[5])); });
+    const at::ScalarType type = dtype(x[5]);
+    Fresh outs(pool);
+    outs.add(x[3], size, type);
+    outs.add(x[4], size, type);
+    const Out k = outs(0, x[3]), v = outs(1, x[4]);
     expect((is_bf16(k.t) || is_f32(k.t)) && plain(k.t, k.t.scalar_type(), size) && plain(v.t, k.t.scalar_type(), size),
            "k_out and v_out are contiguous [tokens, head, head_dim], both bfloat16 or both float32");
     on_current_device(pool, slots, k.t, v.t);
