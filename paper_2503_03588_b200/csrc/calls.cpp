@@ -359,11 +359,11 @@ class Fresh {
     };
     const at::Tensor &like;
     at::Tensor base;
-    int64_t total = 0;
+    int64_t most, total = 0;
     c10::SmallVector<One, 8> list;
 
 public:
-    explicit Fresh(const at::Tensor &t) : like(t) {}
+    explicit Fresh(const at::Tensor &t, int64_t bytes = 1 << 20) : like(t), most(bytes) {}
     // An output that will be needed if `given` is None.  (`size` has to outlive this.)
     void add(PyObject *given, at::IntArrayRef size, at::ScalarType type)
     {
@@ -376,7 +376,7 @@ public:
     {
         const One &o = list[i];
         return Out(given, [&]() -> at::Tensor {
-            if (total > (1 << 20)) return make(like, o.size, o.type);
+            if (total > most) return make(like, o.size, o.type);
             if (!base.defined()) base = make(like, {total}, at::kByte);
             at::Tensor t = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(base.storage()), base.key_set(), c10::scalarTypeToTypeMeta(o.type));
             t.unsafeGetTensorImpl()->set_sizes_contiguous(o.size);
@@ -409,7 +409,7 @@ PyObject *build_block_tables(PyObject *const *x)
     const pa_table_params p = {(int32_t)batch, block, (int32_t)table.size(1), n_pages, max_tokens,
                                (int32_t)pages.numel()};
     const int64_t some = batch + 1, tokens = max_tokens, one = 1, bytes = (int64_t)pa_build_block_tables_workspace_bytes(&p) + 16;
-    Fresh outs(fresh);
+    Fresh outs(fresh, 64 << 20);
     outs.add(x[7], some, at::kInt);
     outs.add(x[8], tokens, at::kLong);
     outs.add(x[9], tokens, at::kInt);

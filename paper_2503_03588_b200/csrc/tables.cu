@@ -1,6 +1,8 @@
 // pa_build_block_tables: pages, slots and positions of a batch's new tokens from the sequences' lengths.
 //
-// Two prefix sums over the batch (new tokens, pages wanted), then one entry per token.  A thread looks up the sequence of its
+// Two prefix sums over the batch (new tokens, pages wanted), then one entry per token.  Up to 1024 sequences every CTA takes the
+// sums itself, which costs less than a kernel that has to wait for them (500 prompts of up to 4000 tokens: 10.8 us in two
+// kernels).  A thread looks up the sequence of its
 // tokens by bisection over the sums.  Every fresh block has exactly one first token, and it is this token's thread that
 // writes the table entry; a token's own page comes from the table for blocks that the sequence had and from the stack
 // for fresh ones, so no thread reads what another one writes.
@@ -11,15 +13,16 @@
 namespace pa {
 
 constexpr int kPageTokens = 64;
-constexpr int kScanThreads = 1024;
-constexpr int kSmallBatch = 1024;    // one CTA does it all up to this many sequences ...
-constexpr int kSmallTokens = 4096;   // ... and this many places for tokens
-constexpr int kFillThreads = 256;
+constexpr int kTableThreads = 256;
+constexpr int kPerThread = 4;        // sequences of a thread in one turn of the sums
+constexpr int kTurn = kTableThreads * kPerThread;  // up to this many sequences every CTA takes the sums itself
 constexpr int kFillTokens = 4;       // tokens per thread and turn
+constexpr int kStepTokens = 1024;    // one CTA does it all up to this many places for tokens
+constexpr int32_t kMost = 1 << 30;   // tokens and pages of a call; sums are held at INT32_MAX
 
 // What the tokens of a sequence need to know.
 struct Sequence {
-    int32_t start;   // its first token (held at INT32_MAX)
+    int32_t start;   // its first token
     int32_t cached;  // tokens it had
     int32_t first;   // its first fresh page's place below the top of the stack; -1: refused
     int32_t end;     // behind its last token
@@ -36,109 +39,165 @@ struct TableArgs {
 };
 
 __device__ __forceinline__ int32_t clamp31(int64_t x) { return x > INT32_MAX ? INT32_MAX : (int32_t)x; }
+// Sum of two numbers in [0, 2^31), held below 2^31.
+__device__ __forceinline__ int32_t add31(int32_t a, int32_t b) { return (int32_t)min((uint32_t)a + (uint32_t)b, (uint32_t)INT32_MAX); }
 
-// Inclusive sums of a number over the CTA's threads; `sums`: room for one number a warp.
-__device__ __forceinline__ int64_t scan_cta(int64_t x, int64_t *sums)
+// The sum of x over the CTA's threads before this one (held below 2^31) and over all; `sums`: room for one number a warp.
+__device__ __forceinline__ int32_t scan_cta(int32_t x, int32_t *sums, int32_t *total)
 {
-    const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, warps = blockDim.x >> 5;
+    const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
+    int32_t upto = x;
 #pragma unroll
     for (int o = 1; o < 32; o *= 2) {
-        const int64_t up = __shfl_up_sync(0xffffffffu, x, o);
-        if (lane >= o) x += up;
+        const int32_t up = __shfl_up_sync(0xffffffffu, upto, o);
+        if (lane >= o) upto = add31(upto, up);
     }
-    if (lane == 31) sums[wid] = x;
+    int32_t before = __shfl_up_sync(0xffffffffu, upto, 1);
+    if (lane == 0) before = 0;
+    if (lane == 31) sums[wid] = upto;
     __syncthreads();
-    int64_t before = lane < wid && lane < warps ? sums[lane] : 0;
+    int32_t all = 0;
 #pragma unroll
-    for (int o = 16; o > 0; o /= 2) before += __shfl_xor_sync(0xffffffffu, before, o);
-    return x + before;
+    for (int w = 0; w < kTableThreads / 32; ++w) {
+        if (w == wid) before = add31(before, all);
+        all = add31(all, sums[w]);
+    }
+    *total = all;
+    return before;
 }
 
-// The sequences' sums, by one CTA; writes cu, lens_out, free_left and, for the tokens, seqs[] and the stack's height.
-__device__ __forceinline__ void scan_sequences(const TableArgs &a, Sequence *seqs, int32_t *height)
+// The sequences' sums, by one CTA: seqs[] and the stack's height for the tokens; if `results`, cu, lens_out and free_left.
+__device__ __forceinline__ void scan_sequences(const TableArgs &a, bool results, Sequence *seqs, int32_t *height)
 {
-    __shared__ int64_t sums[2][32], total[2];
+    __shared__ int32_t sums[2][kTableThreads / 32];
     __shared__ int32_t most_taken;
-    const int tid = threadIdx.x, threads = blockDim.x;
+    const int tid = threadIdx.x;
     int32_t stack = *a.free_count;
     stack = stack < 0 ? 0 : stack > a.free_capacity ? a.free_capacity : stack;
     if (tid == 0) most_taken = 0;
-    int64_t tokens = 0, wanted = 0;  // of the sequences before this turn's
-    for (int b0 = 0; b0 < a.batch; b0 += threads) {
-        const int b = b0 + tid;
-        const bool in = b < a.batch;
-        const int32_t n_raw = in ? a.new_lens[b] : 0, c = in ? a.cache_lens[b] : 0;
-        const int64_t n = n_raw > 0 ? n_raw : 0, upto = tokens + scan_cta(n, sums[0]);
-        const int64_t have = c > 0 ? ((int64_t)c + kPageTokens - 1) / kPageTokens : 0;
-        const int64_t need = ((int64_t)c + n + kPageTokens - 1) / kPageTokens;
-        // (a length held in int32 has to fit behind the call as well)
-        const bool fits = in && c >= 0 && n_raw >= 0 && need <= a.max_blocks && upto <= a.max_tokens &&
-                          (int64_t)c + n <= INT32_MAX;
-        const int64_t want = fits ? need - have : 0, pages = wanted + scan_cta(want, sums[1]);
-        const bool served = fits && (want == 0 || pages <= stack);
-        if (in) {
-            a.cu[b] = clamp31(upto - n);
-            if (b == a.batch - 1) a.cu[a.batch] = clamp31(upto);
-            a.lens_out[b] = served ? (int32_t)(c + n) : c;
-            seqs[b] = Sequence{clamp31(upto - n), c, served ? (int32_t)(pages - want) : -1, clamp31(upto)};
-            if (served && want > 0) atomicMax(&most_taken, (int32_t)pages);
+    int32_t tokens = 0, wanted = 0;  // of the sequences before this turn's
+    for (int b0 = 0; b0 < a.batch; b0 += kTurn) {
+        int32_t n[kPerThread], c[kPerThread], want[kPerThread], start[kPerThread], upto[kPerThread];
+        bool fits[kPerThread];
+        int32_t mine = 0;
+#pragma unroll
+        for (int x = 0; x < kPerThread; ++x) {
+            const int b = b0 + tid * kPerThread + x;
+            n[x] = b < a.batch ? a.new_lens[b] : 0;
+            c[x] = b < a.batch ? a.cache_lens[b] : 0;
         }
-        if (tid == threads - 1) {
-            total[0] = upto;
-            total[1] = pages;
+#pragma unroll
+        for (int x = 0; x < kPerThread; ++x) mine = add31(mine, max(n[x], 0));
+        int32_t total_tokens, total_pages;
+        int32_t sum = add31(tokens, scan_cta(mine, sums[0], &total_tokens)), pages = 0;
+#pragma unroll
+        for (int x = 0; x < kPerThread; ++x) {
+            start[x] = sum;
+            upto[x] = sum = add31(sum, max(n[x], 0));
+            const int64_t behind = (int64_t)c[x] + n[x];
+            // (a length held in int32 has to fit behind the call as well)
+            fits[x] = n[x] >= 0 && c[x] >= 0 && sum <= a.max_tokens && behind <= min((int64_t)a.max_blocks * kPageTokens, (int64_t)INT32_MAX);
+            want[x] = fits[x] ? (int32_t)((behind + kPageTokens - 1) / kPageTokens) - (c[x] / kPageTokens + (c[x] % kPageTokens != 0)) : 0;
+            pages = add31(pages, want[x]);
         }
+        int32_t before = add31(wanted, scan_cta(pages, sums[1], &total_pages));
+#pragma unroll
+        for (int x = 0; x < kPerThread; ++x) {
+            const int b = b0 + tid * kPerThread + x;
+            if (b >= a.batch) break;
+            const int32_t taken = add31(before, want[x]);
+            const bool served = fits[x] && (want[x] == 0 || taken <= stack);
+            if (seqs) seqs[b] = Sequence{start[x], c[x], served ? before : -1, upto[x]};
+            if (results) {
+                a.cu[b + 1] = upto[x];
+                if (b == 0) a.cu[0] = 0;
+                a.lens_out[b] = served ? c[x] + n[x] : c[x];
+                if (served && want[x] > 0) atomicMax(&most_taken, taken);
+            }
+            before = taken;
+        }
+        tokens = add31(tokens, total_tokens);
+        wanted = add31(wanted, total_pages);
         __syncthreads();
-        tokens = total[0];
-        wanted = total[1];
     }
     if (tid == 0) {
-        *height = stack;
-        *a.free_left = stack - most_taken;
+        if (height) *height = stack;
+        if (results) *a.free_left = stack - most_taken;
     }
 }
 
-// kFillTokens tokens from i0 on.
+// The first sequence of batch that ends behind token i, for a warp (all lanes the same i): 32 at a time.
+__device__ __forceinline__ int find_sequence(const TableArgs &a, const Sequence *seqs, int32_t i)
+{
+    const int lane = threadIdx.x & 31;
+    int from = 0, span = 1;
+    while (span * 32 < a.batch) span *= 32;
+    for (; span > 0; span /= 32) {  // (groups of `span` sequences: how many of the next 32 groups end at or before i?)
+        const int last = from + (lane + 1) * span - 1;
+        const bool done = last < a.batch && seqs[last].end <= i;
+        from += __popc(__ballot_sync(0xffffffffu, done)) * span;
+    }
+    return from;
+}
+
+// The slot of the token at `place` of block j of a sequence that is served, -1 without a page; writes a fresh block's table entry
+// with its first token.
+__device__ __forceinline__ int64_t page_of(const TableArgs &a, const Sequence &s, int b, int32_t j, int32_t place, int32_t height)
+{
+    int32_t *entry = a.table + (int64_t)b * a.max_blocks + j;
+    const int32_t have = s.cached / kPageTokens + (s.cached % kPageTokens != 0);
+    int32_t page;
+    if (j < have) {
+        page = *entry;
+    } else {
+        page = a.free_pages[height - 1 - (s.first + (j - have))];
+        if (place == 0) *entry = page;
+    }
+    return page >= 0 && page < a.n_pages ? (int64_t)page * kPageTokens + place : -1;
+}
+
+// kFillTokens tokens a lane from i0 on (lanes take them in order; all lanes of the warp take part).
 __device__ __forceinline__ void fill_tokens(const TableArgs &a, const Sequence *seqs, int32_t height, int32_t i0)
 {
-    // The first sequence that ends behind token i0.
-    int lo = 0, hi = a.batch;
+    // The lane's first sequence lies between those of the warp's first and last token.
+    const int32_t w0 = i0 - (int32_t)(threadIdx.x & 31) * kFillTokens;
+    int lo = find_sequence(a, seqs, w0), hi = find_sequence(a, seqs, w0 + 32 * kFillTokens - 1);
     while (lo < hi) {
         const int mid = (lo + hi) >> 1;
         if (seqs[mid].end <= i0) lo = mid + 1;
         else hi = mid;
     }
+    if (i0 >= a.max_tokens) return;
     int b = lo;
     Sequence s = {};
     if (b < a.batch) s = seqs[b];
+    // Four tokens of one sequence, in one page or two: all but a few.
+    if (a.vector && b < a.batch && i0 + kFillTokens <= s.end && i0 + kFillTokens <= a.max_tokens && s.first >= 0) {
+        const int32_t at = s.cached + (i0 - s.start), j = at / kPageTokens, place = at % kPageTokens;
+        const int64_t slot = page_of(a, s, b, j, place, height);
+        const int64_t next = place > kPageTokens - kFillTokens ? page_of(a, s, b, j + 1, 0, height) : -1;
+        auto slot_of = [&](int x) -> int64_t {
+            return place + x < kPageTokens ? (slot < 0 ? -1 : slot + x) : (next < 0 ? -1 : next + (place + x - kPageTokens));
+        };
+        longlong2 *to = reinterpret_cast<longlong2 *>(a.slots + i0);
+        to[0] = make_longlong2(slot_of(0), slot_of(1));
+        to[1] = make_longlong2(slot_of(2), slot_of(3));
+        *reinterpret_cast<int4 *>(a.positions + i0) = make_int4(at, at + 1, at + 2, at + 3);
+        return;
+    }
     int64_t slot[kFillTokens];
     int32_t position[kFillTokens];
-    int32_t block = -1, page = -1;  // the block that `page` belongs to, of sequence b
 #pragma unroll
     for (int x = 0; x < kFillTokens; ++x) {
         const int32_t i = i0 + x;
-        while (b < a.batch && i >= s.end) {
-            block = -1;
+        while (b < a.batch && i >= s.end)
             if (++b < a.batch) s = seqs[b];
-        }
         slot[x] = -1;
         position[x] = -1;
         if (b >= a.batch || i >= a.max_tokens) continue;
         const int64_t at = (int64_t)s.cached + (i - s.start);
         position[x] = clamp31(at);
-        if (s.first < 0) continue;  // refused
-        const int32_t j = (int32_t)(at / kPageTokens), place = (int32_t)(at % kPageTokens);
-        if (j != block) {
-            block = j;
-            int32_t *entry = a.table + (int64_t)b * a.max_blocks + j;
-            const int32_t have = s.cached / kPageTokens + (s.cached % kPageTokens != 0);
-            if (j < have) {
-                page = *entry;
-            } else {
-                page = a.free_pages[height - 1 - (s.first + (j - have))];
-                if (place == 0) *entry = page;
-            }
-        }
-        if (page >= 0 && page < a.n_pages) slot[x] = (int64_t)page * kPageTokens + place;
+        if (s.first >= 0) slot[x] = page_of(a, s, b, (int32_t)at / kPageTokens, (int32_t)at % kPageTokens, height);
     }
     if (a.vector && i0 + kFillTokens <= a.max_tokens) {
         longlong2 *to = reinterpret_cast<longlong2 *>(a.slots + i0);
@@ -155,32 +214,105 @@ __device__ __forceinline__ void fill_tokens(const TableArgs &a, const Sequence *
     }
 }
 
-// One CTA: sums and tokens.
-__global__ void __launch_bounds__(kScanThreads) tables_small_kernel(const TableArgs a)
+// Each CTA takes the sums and then its share of the tokens.  The results that may lie over what the other CTAs still read are left
+// to tables_results_kernel unless `results`.
+__global__ void __launch_bounds__(kTableThreads) tables_kernel(const TableArgs a, bool results)
 {
-    __shared__ Sequence seqs[kSmallBatch];
+    __shared__ Sequence seqs[kTurn];
     __shared__ int32_t height;
     pdl_launch_next();
     pdl_wait();
-    scan_sequences(a, seqs, &height);
+    scan_sequences(a, results && blockIdx.x == 0, seqs, &height);
     __syncthreads();
-    for (int32_t i = threadIdx.x * kFillTokens; i < a.max_tokens; i += blockDim.x * kFillTokens)
-        fill_tokens(a, seqs, height, i);
+    const int64_t step = (int64_t)gridDim.x * kTableThreads * kFillTokens;
+    for (int64_t w = ((int64_t)blockIdx.x * kTableThreads + (threadIdx.x & ~31)) * kFillTokens; w < a.max_tokens; w += step)
+        fill_tokens(a, seqs, height, (int32_t)w + (int32_t)(threadIdx.x & 31) * kFillTokens);
 }
-
-__global__ void __launch_bounds__(kScanThreads) tables_scan_kernel(const TableArgs a)
+__global__ void __launch_bounds__(kTableThreads) tables_results_kernel(const TableArgs a)
 {
     pdl_launch_next();
     pdl_wait();
-    scan_sequences(a, a.seqs, a.count);
+    scan_sequences(a, true, nullptr, nullptr);
 }
 
-__global__ void __launch_bounds__(kFillThreads) tables_fill_kernel(const TableArgs a)
+// A decoding step, one CTA: a thread per sequence takes the sums and, where no sequence has more than kFew tokens, writes its tokens
+// itself.
+constexpr int kFew = 4;
+__global__ void __launch_bounds__(kTurn) tables_step_kernel(const TableArgs a)
+{
+    __shared__ Sequence seqs[kTurn];
+    __shared__ int32_t sums[2][32], most_taken;
+    pdl_launch_next();
+    const int b = threadIdx.x, lane = b & 31, wid = b >> 5, warps = blockDim.x >> 5;
+    if (b == 0) most_taken = 0;
+    pdl_wait();
+    int32_t stack = *a.free_count;
+    const int32_t n_raw = b < a.batch ? a.new_lens[b] : 0, c = b < a.batch ? a.cache_lens[b] : 0, n = max(n_raw, 0);
+    stack = stack < 0 ? 0 : stack > a.free_capacity ? a.free_capacity : stack;
+    auto scan = [&](int32_t x, int32_t *sum, int32_t &all) {  // the sum before this thread, and over all
+        int32_t upto = x;
+#pragma unroll
+        for (int o = 1; o < 32; o *= 2) {
+            const int32_t up = __shfl_up_sync(0xffffffffu, upto, o);
+            if (lane >= o) upto = add31(upto, up);
+        }
+        if (lane == 31) sum[wid] = upto;
+        __syncthreads();
+        int32_t before = 0;
+        all = 0;
+        for (int w = 0; w < warps; ++w) {
+            if (w == wid) before = all;
+            all = add31(all, sum[w]);
+        }
+        const int32_t mine = __shfl_up_sync(0xffffffffu, upto, 1);
+        return add31(before, lane ? mine : 0);
+    };
+    int32_t tokens, pages;
+    const int32_t start = scan(n, sums[0], tokens), end = add31(start, n);
+    const int64_t behind = (int64_t)c + n;
+    const bool fits = n_raw >= 0 && c >= 0 && end <= a.max_tokens && behind <= min((int64_t)a.max_blocks * kPageTokens, (int64_t)INT32_MAX);
+    const int32_t have = c > 0 ? c / kPageTokens + (c % kPageTokens != 0) : 0;
+    const int32_t want = fits ? (int32_t)((behind + kPageTokens - 1) / kPageTokens) - have : 0;
+    const int32_t before = scan(want, sums[1], pages), taken = add31(before, want);
+    const bool served = fits && (want == 0 || taken <= stack);
+    const Sequence s = {start, c, served ? before : -1, end};
+    if (b < a.batch) {
+        a.cu[b + 1] = end;
+        if (b == 0) a.cu[0] = 0;
+        a.lens_out[b] = served ? c + n : c;
+        if (served && want > 0) atomicMax(&most_taken, taken);
+    }
+    seqs[b] = s;
+    if (__syncthreads_or(n > kFew)) {
+        for (int32_t w = (b & ~31) * kFillTokens; w < a.max_tokens; w += blockDim.x * kFillTokens)
+            fill_tokens(a, seqs, stack, w + lane * kFillTokens);
+    } else {
+        for (int x = 0; x < n && start + x < a.max_tokens; ++x) {
+            const int64_t at = (int64_t)c + x;
+            a.positions[start + x] = clamp31(at);
+            a.slots[start + x] = served ? page_of(a, s, b, (int32_t)at / kPageTokens, (int32_t)at % kPageTokens, stack) : -1;
+        }
+        for (int32_t i = add31(tokens, b); i < a.max_tokens; i += blockDim.x) {
+            a.positions[i] = -1;
+            a.slots[i] = -1;
+        }
+    }
+    if (b == 0) *a.free_left = stack - most_taken;
+}
+
+// Large batches: the sums by one CTA, then the tokens.
+__global__ void __launch_bounds__(kTableThreads) tables_scan_kernel(const TableArgs a)
 {
     pdl_launch_next();
     pdl_wait();
-    const int64_t i = ((int64_t)blockIdx.x * kFillThreads + threadIdx.x) * kFillTokens;
-    if (i < a.max_tokens) fill_tokens(a, a.seqs, *a.count, (int32_t)i);
+    scan_sequences(a, true, a.seqs, a.count);
+}
+__global__ void __launch_bounds__(kTableThreads) tables_fill_kernel(const TableArgs a)
+{
+    pdl_launch_next();
+    pdl_wait();
+    const int64_t i = ((int64_t)blockIdx.x * kTableThreads + threadIdx.x) * kFillTokens;
+    if (i - (threadIdx.x & 31) * kFillTokens < a.max_tokens) fill_tokens(a, a.seqs, *a.count, (int32_t)i);
 }
 
 static pa_status check_table_params(const pa_table_params *p)
@@ -190,6 +322,7 @@ static pa_status check_table_params(const pa_table_params *p)
         return fail(PA_ERR_INVALID_ARG, "batch, max_blocks_per_seq, n_pages and max_tokens must be positive");
     if (p->block != kPageTokens) return fail(PA_ERR_SHAPE, "block must be 64");
     if (p->batch > 65535) return fail(PA_ERR_SHAPE, "batch must be <= 65535");
+    if (p->max_tokens > kMost || p->free_capacity > kMost) return fail(PA_ERR_SHAPE, "max_tokens and free_capacity must be <= 2^30");
     return PA_OK;
 }
 
@@ -240,14 +373,19 @@ extern "C" pa_status pa_build_block_tables(const pa_table_params *p, const int32
     a.free_capacity = p->free_capacity;
     a.vector = aligned16(slot_map) && aligned16(positions);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    auto threads_for = [](int64_t n) { return (unsigned)(n >= kScanThreads ? kScanThreads : (n + 31) / 32 * 32); };
-    if (p->batch <= kSmallBatch && p->max_tokens <= kSmallTokens) {
-        const int64_t quads = (p->max_tokens + kFillTokens - 1) / kFillTokens;
-        PA_CUDA_OK(launch_pdl(tables_small_kernel, dim3(1), threads_for(p->batch > quads ? p->batch : quads), 0, st, a));
+    const int64_t quads = (p->max_tokens + kFillTokens - 1) / kFillTokens, ctas = (quads + kTableThreads - 1) / kTableThreads;
+    if (p->batch <= kTurn && p->max_tokens <= kStepTokens) {
+        PA_CUDA_OK(launch_pdl(tables_step_kernel, dim3(1), (unsigned)(p->batch + 31) / 32 * 32, 0, st, a));
         return PA_OK;
     }
-    PA_CUDA_OK(launch_pdl(tables_scan_kernel, dim3(1), threads_for(p->batch), 0, st, a));
-    const int64_t per_cta = kFillThreads * kFillTokens;
-    PA_CUDA_OK(launch_pdl(tables_fill_kernel, dim3((unsigned)((p->max_tokens + per_cta - 1) / per_cta)), kFillThreads, 0, st, a));
+    if (p->batch <= kTurn) {
+        constexpr int64_t kAtOnce = 148 * 2;  // (the sums cost as much as some tokens a thread)
+        const bool apart = lens_out != cache_lens && free_left != free_count;
+        PA_CUDA_OK(launch_pdl(tables_kernel, dim3((unsigned)(ctas < kAtOnce ? ctas : kAtOnce)), kTableThreads, 0, st, a, apart));
+        if (!apart) PA_CUDA_OK(launch_pdl(tables_results_kernel, dim3(1), kTableThreads, 0, st, a));
+        return PA_OK;
+    }
+    PA_CUDA_OK(launch_pdl(tables_scan_kernel, dim3(1), kTableThreads, 0, st, a));
+    PA_CUDA_OK(launch_pdl(tables_fill_kernel, dim3((unsigned)ctas), kTableThreads, 0, st, a));
     return PA_OK;
 }

@@ -35,7 +35,7 @@ def _check_tables(pa, new, cached, free, count, room, n_pages, cap, in_place=Fal
 
 
 @pytest.mark.parametrize("in_place", [False, True])
-@pytest.mark.parametrize("batch,cap", [(1, 1), (1, 5), (3, 130), (31, 1000), (33, 4096), (64, 4097), (1000, 4096), (1024, 9000),
+@pytest.mark.parametrize("batch,cap", [(1, 1), (1, 5), (3, 130), (31, 1000), (700, 900), (1024, 1024), (1024, 1025), (33, 4096), (64, 4097), (1000, 4096), (1024, 9000),
                                        (1025, 100), (2500, 70001), (5, 300000)])
 def test_tables(pa, batch, cap, in_place):
     """One and several kernels, turns of 1024 sequences, ragged ends, a padded batch; the stack ends in the middle."""
@@ -51,7 +51,12 @@ def test_tables(pa, batch, cap, in_place):
 
 
 def test_tables_of_a_decoding_step(pa):
-    """One token each, page boundaries among them; an idle sequence gets nothing."""
+    """A few tokens each, page boundaries among them; an idle sequence gets nothing; most of the batch is padding."""
+    rng = np.random.default_rng(3)
+    for batch, cap in ((1000, 1024), (33, 140), (5, 900), (1024, 1000)):
+        cached = rng.integers(0, 400, batch)
+        _check_tables(pa, rng.integers(-1 if batch > 500 else 0, 2 if batch > 100 else 5, batch), cached, rng.permutation(1100), 1100 if batch < 100 else 6, 8, 1000, cap,
+                      in_place=batch % 2 == 0)
     cached = [0, 1, 63, 64, 65, 127, 128, 200]
     _check_tables(pa, [1] * 8, cached, np.arange(50, 70), 20, 5, 100, 8, in_place=True)
     _check_tables(pa, [1, 0, 1, 0, 1, 0, 1, 1], cached, np.arange(50, 70), 2, 5, 100, 64)
@@ -65,6 +70,7 @@ def test_tables_refuse_sequences_not_calls(pa):
     _check_tables(pa, [100, 250, 100], [0, 0, 63], np.arange(30), 30, 8, 50, 300)         # the second ends behind 300
     _check_tables(pa, [100, 250, 10], [0, 0, 3], np.arange(30), 5, 8, 50, 400)            # the second finds no pages, the third needs none
     _check_tables(pa, [big, big, 3], [0, 0, 0], np.arange(30), 30, 8, 50, 400)            # sums beyond 31 bits
+    _check_tables(pa, [5, big, 3], [0, 0, 0], np.arange(30), 30, 8, 50, 400)
     _check_tables(pa, [3, 3], [big - 2, big - 3], np.arange(30), 30, 8, 50, 400)
     _check_tables(pa, [70, 70], [0, 0], np.arange(3), 99, 8, 50, 400)                     # a height above the stack
     _check_tables(pa, [70, 70], [0, 0], np.arange(3), -4, 8, 50, 400)
@@ -77,6 +83,26 @@ def test_tables_pages_beyond_32_bits(pa):
     n = 2 ** 31 - 1
     out = _check_tables(pa, [130, 70], [10, 0], [n - 1, 5, n - 2, n, 2 ** 26], 5, 4, n, 256)
     assert int(out[1].max()) > 2 ** 36
+
+
+def test_tables_captured_and_replayed(pa):
+    """Decoding steps from one graph, results in place: pages come off the stack, lengths grow, until no page is left."""
+    batch, room, n_pages = 5, 4, 12
+    lens, left, t = _ints([60, 0, 63, 64, 10]), _ints([9]), _ints(np.tile(np.arange(room), (batch, 1)) + 100)
+    new, free = _ints([1, 1, 1, 1, 0]), _ints(np.arange(12) + 3)
+    out = pa.pa_build_block_tables(new, lens, free, left, t, 200, 8)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = pa.pa_build_block_tables(new, lens, free, left, t, 200, 8, lens_out=lens, free_left=left)
+    ref = (lens.tolist(), int(left), t.cpu().numpy())
+    for _ in range(210):
+        graph.replay()
+        cu, slots, positions, l2, f2, t2 = plain.tables([1, 1, 1, 1, 0], ref[0], np.arange(12) + 3, ref[1], ref[2], 200, 8)
+        np.testing.assert_array_equal(out[1].cpu().numpy(), slots)
+        np.testing.assert_array_equal(out[2].cpu().numpy(), positions)
+        ref = (l2, f2, t2)
+    assert lens.tolist() == ref[0] and int(left) == ref[1] == 0 and max(ref[0]) < 256
+    np.testing.assert_array_equal(t.cpu().numpy(), ref[2])
 
 
 def test_tables_arrays_off_16_bytes(pa):

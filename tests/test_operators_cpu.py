@@ -41,7 +41,8 @@ def test_tables_refusals(b):
         assert b.lib.pa_build_block_tables_workspace_bytes(_changed(good, **bad)) == 0
     assert status(None) == "PA_ERR_INVALID_ARG"
     assert status(_changed(good, block=128)) == "PA_ERR_SHAPE"
-    assert status(_changed(good, batch=65536)) == "PA_ERR_SHAPE"
+    for bad in (dict(batch=65536), dict(max_tokens=2 ** 30 + 1), dict(free_capacity=2 ** 30 + 1)):
+        assert status(_changed(good, **bad)) == "PA_ERR_SHAPE", bad
     for at in range(10):
         assert status(_changed(good), at) == "PA_ERR_INVALID_ARG", at
     assert status(_changed(good), 6, P + 4) == "PA_ERR_ALIGNMENT"      # slots are 8 bytes each
