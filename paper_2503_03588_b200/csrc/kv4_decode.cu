@@ -52,7 +52,7 @@ struct Kv4Args {
     float *lse;
     int64_t page_stride, head_stride, max_len;
     int32_t table_stride, n_pages, batch, Hkv, G, W, S, R, stages, clear_status;
-    int32_t whole_rows;  // (range kernel) a CTA's range begins and ends with rows; R > 1: that of a cluster of R CTAs does
+    int32_t whole_rows;  // (range kernel) ranges begin and end with rows
     float scale_log2;
     long long wait_cycles;
 };
@@ -647,14 +647,12 @@ __global__ void __launch_bounds__(kC4Threads, 2) kv4_cluster_kernel(const Kv4Arg
 // one is free.  A row that lies in a warp's range from end to end is written from its registers; of the others it keeps
 // the first in shared memory and the last in its registers, and behind a barrier the CTA's warps merge these.  A row that
 // other CTAs have parts of goes to the workspace, where kv4_join_kernel merges it.
-// Where CTAs have many rows, ranges are rounded to whole rows instead, and nothing is left for the second kernel; where they
-// have few, clusters of CTAs take ranges of whole rows and share them out evenly, their parts in shared memory.
+// Where no row is long, ranges are rounded to whole rows instead, and nothing is left for the second kernel.
 // The ranges follow from the lengths, which are on the device: each CTA sums all sequences' blocks up (a thread takes
 // batch / 384 of them), and each thread looks one block of the CTA's range up.
 // ------------------------------------------------------------------------------------------
 constexpr int kR4Warps = 12;
 constexpr int kR4Threads = 32 * kR4Warps;
-constexpr int kR4Cluster = 4;        // CTAs that share rows
 constexpr int kR4Ctas = 148;         // CTAs, times a number that keeps every range at no more than a block per thread
 
 template <int D>
@@ -670,8 +668,7 @@ struct Kv4RangeSmem {
     static constexpr uint32_t kDesc = (kBars + kR4Warps * kHalves * 8 + 15) & ~15u;
     static constexpr uint32_t kSums = kDesc + kR4Threads * 16;
     static constexpr uint32_t kIds = kSums + kR4Threads * 8;      // rows of the pieces, int32 [warps][2]; the abort flag
-    static constexpr uint32_t kParts = kIds + 2 * kR4Warps * 4 + 16;    // (clusters) the CTA's two parts
-    static constexpr size_t bytes(bool cluster) { return 128 + kParts + (cluster ? 2 * (4 + 2 * kD4MaxGroup + kD4MaxGroup * D) * 4 : 0); }
+    static constexpr size_t bytes() { return 128 + kIds + 2 * kR4Warps * 4 + 16; }
 };
 
 // A row's result in the workspace: its number (-1: none; -2: the CTA has no blocks), then eight heads' maxima, sums and outputs.
@@ -745,61 +742,36 @@ __global__ void __launch_bounds__(kR4Threads, 1) kv4_range_kernel(const Kv4Args 
         total += v;
     }
     sums[tid] = make_int2(before + upto - mine, my_len);
+    const int32_t lo = (int32_t)((int64_t)total * blockIdx.x / gridDim.x), hi = (int32_t)((int64_t)total * (blockIdx.x + 1) / gridDim.x);
     __syncthreads();
-    struct Block {
-        LayoutRowOf<int32_t> r;
-        int32_t b, hk, i, len;  // sequence, KV head, number in the row; the sequence's length
-    };
-    auto find = [&](int32_t x) {  // block x of all rows' blocks
-        Block f;
-        int k = 0, end = kR4Threads;  // the last k whose sequences begin at or before it
-        while (end - k > 1) {
-            const int mid = (k + end) >> 1;
-            if (sums[mid].x <= x) k = mid;
-            else end = mid;
-        }
-        int32_t at = x - sums[k].x;
-        f.len = per == 1 ? sums[k].y : len_of(k * per);
-        f.b = k * per;
-        f.r = row_of(f.len);
-        while (at >= f.r.n * a.Hkv) {
-            at -= f.r.n * a.Hkv;
-            f.len = len_of(++f.b);
-            f.r = row_of(f.len);
-        }
-        f.hk = at / f.r.n;
-        f.i = at - f.hk * f.r.n;
-        return f;
-    };
-    const int R = a.R;
-    const unsigned rank = blockIdx.x % (unsigned)R, cluster = blockIdx.x / (unsigned)R, clusters = gridDim.x / (unsigned)R;
-    int32_t lo = (int32_t)((int64_t)total * cluster / clusters), hi = (int32_t)((int64_t)total * (cluster + 1) / clusters);
-    if (R > 1) {  // up to the next row's begin, then this CTA's share
-        int32_t x = lane & 1 ? hi : lo;
-        if (lane < 2 && x < total) {
-            const Block f = find(x);
-            if (f.i) x += f.r.n - f.i;
-        }
-        lo = __shfl_sync(0xffffffffu, x, 0);
-        const int32_t all = __shfl_sync(0xffffffffu, x, 1) - lo;
-        hi = lo + (int32_t)((int64_t)all * (rank + 1) / R);
-        lo += (int32_t)((int64_t)all * rank / R);
-    }
 
     // ---- Thread: block lo + tid.  It belongs to the range if it lies in [lo, hi), or if its row begins there (whole_rows).
     bool inside = false, earlier = false;
     int4 found = make_int4(0, 0, 0, 0);
     if (lo + tid < (a.whole_rows ? total : hi)) {
-        const Block f = find(lo + tid);
-        const int32_t begin = lo + tid - f.i;
+        int k = 0, end = kR4Threads;  // the last k whose sequences begin at or before this block
+        while (end - k > 1) {
+            const int mid = (k + end) >> 1;
+            if (sums[mid].x <= lo + tid) k = mid;
+            else end = mid;
+        }
+        int32_t at = lo + tid - sums[k].x, len = per == 1 ? sums[k].y : len_of(k * per);
+        int b = k * per;
+        LayoutRowOf<int32_t> r = row_of(len);
+        while (at >= r.n * a.Hkv) {
+            at -= r.n * a.Hkv;
+            len = len_of(++b);
+            r = row_of(len);
+        }
+        const int32_t hk = at / r.n, i = at - hk * r.n, begin = lo + tid - i;
         earlier = a.whole_rows && begin < lo;
         inside = !a.whole_rows || (begin >= lo && begin < hi);
         if (inside) {
-            int32_t page = a.table[(int64_t)f.b * a.table_stride + layout_entry<int32_t>(f.r, f.i)];
+            int32_t page = a.table[(int64_t)b * a.table_stride + layout_entry<int32_t>(r, i)];
             page = page < 0 ? 0 : page >= a.n_pages ? a.n_pages - 1 : page;
-            const int32_t keys = f.i == f.r.n - 1 ? (f.len - 1) % kKv4Page + 1 : kKv4Page;
-            const int64_t src = (int64_t)page * a.page_stride + (int64_t)f.hk * a.head_stride;
-            found = make_int4((int)(uint32_t)src, (int)(src >> 32), f.b * a.Hkv + f.hk, (f.r.n - f.i) | (keys - 1) << 24 | (f.i == 0) << 30);
+            const int32_t keys = i == r.n - 1 ? (len - 1) % kKv4Page + 1 : kKv4Page;
+            const int64_t src = (int64_t)page * a.page_stride + (int64_t)hk * a.head_stride;
+            found = make_int4((int)(uint32_t)src, (int)(src >> 32), b * a.Hkv + hk, (r.n - i) | (keys - 1) << 24 | (i == 0) << 30);
         }
     }
     const int skipped = a.whole_rows ? __syncthreads_count(earlier) : 0;  // (the first ones)
@@ -922,20 +894,17 @@ __global__ void __launch_bounds__(kR4Threads, 1) kv4_range_kernel(const Kv4Args 
         if (lane == 0) ids[2 * wid + 1] = desc[last - 1].z;
     }
     __syncthreads();
-    const bool aborted = *abort_flag != 0;
-    if (aborted) {
+    if (*abort_flag) {
         if (tid == 0) {  // copies that may still be in flight have a bounded time to land
             const long long t0 = clock64();
             while (clock64() - t0 < 2000000ll) {
             }
         }
-        if (R == 1) return;
-        if (tid < 2 * kR4Warps) ids[tid] = -1;  // (peers will look here: nothing to merge)
-        __syncthreads();
+        return;
     }
 
     // ---- Pieces of the same row follow one another: a run of them.  Warp: a run, or where there are few, some heads of one.
-    float *parts = R > 1 ? reinterpret_cast<float *>(base + SM::kParts) : a.parts + (int64_t)blockIdx.x * 2 * Kv4Part<D>::kFloats;
+    float *parts = a.parts + (int64_t)blockIdx.x * 2 * Kv4Part<D>::kFloats;
     const int32_t row_first = count ? desc[0].z : -1, row_last = count ? desc[count - 1].z : -1;
     const bool open_first = count && !(desc[0].w >> 30), open_last = count && (desc[count - 1].w & 0xffffff) != 1;
     static_assert(2 * kR4Warps <= 32, "a lane per piece");
@@ -1012,58 +981,8 @@ __global__ void __launch_bounds__(kR4Threads, 1) kv4_range_kernel(const Kv4Args 
     else if (wid < 4 * runs)
         merge(std::integral_constant<int, 2>(), wid, 4);
     if (tid < 2 && !a.whole_rows) {
-        const bool there = !aborted && (tid == 0 ? open_first : open_last && !(open_first && row_first == row_last));
+        const bool there = tid == 0 ? open_first : open_last && !(open_first && row_first == row_last);
         reinterpret_cast<int32_t *>(parts + tid * Kv4Part<D>::kFloats)[0] = there ? (tid == 0 ? row_first : row_last) : count ? -1 : -2;
-    }
-
-    // ---- Rows that CTAs of the cluster have parts of: the CTA in which they begin.  Warp: a head; lane: a CTA, then four features.
-    if (R > 1) {
-        ptx::cluster_arrive();
-        ptx::cluster_wait();
-        const uint32_t mine_at = smem + SM::kParts, part_at = mine_at + Kv4Part<D>::kFloats * 4u;
-        const int32_t row = (int32_t)ptx::ld_shared(part_at);
-        for (int h = wid; row >= 0 && h < G; h += kR4Warps) {
-            const unsigned peer = rank + 1 + lane;
-            const bool exists = peer < (unsigned)R;
-            const uint32_t theirs = ptx::map_shared(mine_at, exists ? peer : rank);
-            const int32_t id = exists ? (int32_t)ptx::ld_cluster(theirs) : -1;
-            const uint32_t others = __ballot_sync(0xffffffffu, id != row && id != -2);  // (never empty: 32 > R)
-            const uint32_t mask = __ballot_sync(0xffffffffu, id == row) & ((1u << (__ffs(others) - 1)) - 1u);
-            float mp = -INFINITY, lp = 0.f;
-            if (mask >> lane & 1u) {
-                mp = __uint_as_float(ptx::ld_cluster(theirs + 4u * (4 + 2 * h)));
-                lp = __uint_as_float(ptx::ld_cluster(theirs + 4u * (5 + 2 * h)));
-            }
-            float m, l;
-            ptx::ld_shared_v2(part_at + 4u * (4 + 2 * h), m, l);
-            float top = mp;
-#pragma unroll
-            for (int o = 16; o > 0; o /= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-            top = fmaxf(top, m);
-            const float w0 = m != -INFINITY ? ptx::ex2(m - top) : 0.f, w = mp != -INFINITY ? ptx::ex2(mp - top) : 0.f;
-            lp *= w;
-#pragma unroll
-            for (int o = 16; o > 0; o /= 2) lp += __shfl_xor_sync(0xffffffffu, lp, o);
-            l = fmaf(l, w0, lp);
-            const uint32_t features = 4u * (4 + 2 * kD4MaxGroup + h * D + 4 * lane);
-            float4 out = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (4 * lane < D) {
-                float4 v;
-                ptx::ld_shared_v4(part_at + features, v.x, v.y, v.z, v.w);
-                add_part(out, v, w0);
-            }
-            for (uint32_t left = mask; left; left &= left - 1) {
-                const int p = __ffs(left) - 1;
-                const float wp = __shfl_sync(0xffffffffu, w, p);
-                if (4 * lane < D) add_part(out, ptx::ld_cluster_v4(ptx::map_shared(mine_at, rank + 1 + p) + features), wp);
-            }
-            const int64_t head = (int64_t)row * G + h;
-            if (4 * lane < D) write4<kF32>(a.o, head * D + 4 * lane, out, 1.0f / l);
-            if (lane == 0) a.lse[head] = natural(top, l);
-        }
-        ptx::cluster_arrive();  // (no CTA leaves while another one reads its parts)
-        ptx::cluster_wait();
-        if (aborted) return;
     }
 
     // ---- Sequences without a key (a length outside [1, max_len]): zeros.
@@ -1177,12 +1096,17 @@ static pa_status check_kv4(const pa_kv4_params *p)
     return PA_OK;
 }
 
-// CTAs of the range kernel where a row may have parts in several: no range is longer than a block per thread, whatever the lengths
-// are.
+// Whether ranges are rounded to whole rows: where a row is worth less than the second kernel, and CTAs have many.
+static bool kv4_whole_rows(const pa_kv4_params *p)
+{
+    return kv4_most_blocks(p) <= 24 && (int64_t)p->batch * p->pool.n_kv_heads >= 2 * kR4Ctas;
+}
+// CTAs of the range kernel: no range, rounded or not, is longer than a block per thread, whatever the lengths are.
 static int64_t kv4_range_ctas(const pa_kv4_params *p)
 {
-    const int64_t blocks = (int64_t)p->batch * p->pool.n_kv_heads * kv4_most_blocks(p);
-    const int64_t turns = (blocks + kR4Ctas * kR4Threads - 1) / (kR4Ctas * kR4Threads);
+    const int64_t most = kv4_most_blocks(p), blocks = (int64_t)p->batch * p->pool.n_kv_heads * most;
+    const int64_t room = kv4_whole_rows(p) ? kR4Threads - 2 * most : kR4Threads;
+    const int64_t turns = (blocks + kR4Ctas * room - 1) / (kR4Ctas * room);
     return turns * kR4Ctas;
 }
 
@@ -1197,17 +1121,12 @@ static Kv4Kernel kv4_kernel(int head_dim, bool f32, int which)
          {kv4_cluster_kernel<128, true>, kv4_range_kernel<128, true>, kv4_join_kernel<128, true>}}};
     return kernels[head_dim == 128][f32][which];
 }
-static size_t kv4_range_smem(int head_dim, bool cluster)
-{
-    return head_dim == 128 ? Kv4RangeSmem<128>::bytes(cluster) : Kv4RangeSmem<64>::bytes(cluster);
-}
 static size_t kv4_cluster_smem(int head_dim, int stages)
 {
     return head_dim == 128 ? Kv4ClusterSmem<128>::bytes(stages) : Kv4ClusterSmem<64>::bytes(stages);
 }
 
-// How many clusters of R CTAs of the cluster kernel (stages > 0) or the range kernel (0) the device holds at once.  Asked once per
-// device and kind of launch.
+// How many clusters of R CTAs the device holds at once.  Asked once per device and kind of launch.
 static pa_status kv4_resident_clusters(int device, int head_dim, bool f32, int stages, int R, int *out)
 {
     static std::mutex mu;
@@ -1222,12 +1141,12 @@ static pa_status kv4_resident_clusters(int device, int head_dim, bool f32, int s
         attr.val.clusterDim.z = 1;
         cudaLaunchConfig_t cfg = {};
         cfg.gridDim = dim3((unsigned)R, 1, 1);
-        cfg.blockDim = dim3(stages ? kC4Threads : kR4Threads, 1, 1);
-        cfg.dynamicSmemBytes = stages ? kv4_cluster_smem(head_dim, stages) : kv4_range_smem(head_dim, true);
+        cfg.blockDim = dim3(kC4Threads, 1, 1);
+        cfg.dynamicSmemBytes = kv4_cluster_smem(head_dim, stages);
         cfg.attrs = &attr;
         cfg.numAttrs = 1;
         int found = 0;
-        PA_CUDA_OK(cudaOccupancyMaxActiveClusters(&found, kv4_kernel(head_dim, f32, stages ? 0 : 1), &cfg));
+        PA_CUDA_OK(cudaOccupancyMaxActiveClusters(&found, kv4_kernel(head_dim, f32, 0), &cfg));
         n = found + 1;
     }
     *out = n - 1;
@@ -1342,43 +1261,12 @@ extern "C" pa_status pa_decode_kv4(const pa_kv4_params *p, const void *q, const 
         PA_CUDA_OK(cudaLaunchKernelEx(&cfg, kv4_kernel(D, f32, 0), a));
         return PA_OK;
     }
-    // Ranges: of whole rows where a CTA has at least two of them and none is long, else of whole rows per cluster where that has two
-    // of them, else as they fall.
-    const bool spread = env.decode_path == 1;  // (the last of these, for tests)
-    a.stages = 0;
     a.R = 1;
-    a.whole_rows = !spread && most <= 24 && rows >= 2 * kR4Ctas;
-    int64_t ctas = kv4_range_ctas(p);
-    if (!spread && !a.whole_rows) {
-        const int shares = env.decode_cluster ? env.decode_cluster : kR4Cluster;
-        int fit = 0;
-        if (shares > 1)
-            if (pa_status s = kv4_resident_clusters(dev.device, D, f32, 0, shares, &fit)) return s;
-        const int64_t room = (int64_t)shares * (kR4Threads - 1) - 2 * most;  // blocks of a cluster's range before it is rounded
-        if (fit > 0 && room > most && rows >= 2 * fit) {
-            const int64_t turns = (rows * most + fit * room - 1) / (fit * room);
-            a.R = shares;
-            ctas = turns * fit * shares;
-        }
-    }
-    if (a.whole_rows) {
-        const int64_t room = kR4Threads - 2 * most, turns = (rows * most + kR4Ctas * room - 1) / (kR4Ctas * room);
-        ctas = turns * kR4Ctas;
-    }
-    cudaLaunchAttribute attr[2];
-    attr[0] = pdl_attribute();
-    attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = (unsigned)a.R;
-    attr[1].val.clusterDim.y = 1;
-    attr[1].val.clusterDim.z = 1;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)ctas, 1, 1);
-    cfg.blockDim = dim3(kR4Threads, 1, 1);
-    cfg.dynamicSmemBytes = kv4_range_smem(D, a.R > 1);
-    cfg.stream = st;
-    cfg.attrs = attr;
-    cfg.numAttrs = a.R > 1 ? 2 : 1;
-    PA_CUDA_OK(cudaLaunchKernelEx(&cfg, kv4_kernel(D, f32, 1), a));
-    if (!a.whole_rows && a.R == 1) PA_CUDA_OK(launch_pdl(kv4_kernel(D, f32, 2), dim3((unsigned)ctas), kJ4Threads, 0, st, a));
+    a.stages = 0;
+    a.whole_rows = kv4_whole_rows(p);
+    const unsigned ctas = (unsigned)kv4_range_ctas(p);
+    const size_t smem = D == 128 ? Kv4RangeSmem<128>::bytes() : Kv4RangeSmem<64>::bytes();
+    PA_CUDA_OK(launch_pdl(kv4_kernel(D, f32, 1), dim3(ctas), kR4Threads, smem, st, a));
+    if (!a.whole_rows) PA_CUDA_OK(launch_pdl(kv4_kernel(D, f32, 2), dim3(ctas), kJ4Threads, 0, st, a));
     return PA_OK;
 }

@@ -398,20 +398,6 @@ __device__ __forceinline__ void st_async_v4(uint32_t addr, const float4 &v, uint
                  : "memory");
 }
 
-// From the shared memory of a CTA of the cluster (an address by map_shared).
-__device__ __forceinline__ uint32_t ld_cluster(uint32_t addr)
-{
-    uint32_t v;
-    asm volatile("ld.shared::cluster.u32 %0, [%1];\n" : "=r"(v) : "r"(addr) : "memory");
-    return v;
-}
-__device__ __forceinline__ float4 ld_cluster_v4(uint32_t addr)
-{
-    float4 v;
-    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];\n" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
-    return v;
-}
-
 __device__ __forceinline__ float ex2(float x)
 {
     float y;

@@ -230,36 +230,18 @@ def test_decode_kv4_many_rows(pa, oracle, pa_env):
     c.check(oracle, 16, 5, 1)
     c = _Cache(pa, lens, 4, 128, seed=6)
     c.check(oracle, 28, 9, 1, torch.float32)
+    pa_env(PA_DECODE_PATH="persist")
+    c = _Cache(pa, lens[:40], 1, 64, seed=14)
+    c.check(oracle, 1, 5, 1)
+    c = _Cache(pa, [300, 0, 64, 1, -1, 129], 1, 128, seed=15)
+    c.check(oracle, 8, 5, 1, torch.float32)
+    c = _Cache(pa, [0, 0], 2, 64, seed=16)
+    c.check(oracle, 8, 5, 1)
     short = [int(x) for x in np.random.default_rng(5).integers(-20, 200, 1000)]
-    for path in ("persist", "splitk"):
-        pa_env(PA_DECODE_PATH=path)
-        c = _Cache(pa, lens[:40], 1, 64, seed=14)
-        c.check(oracle, 1, 5, 1)
-        c = _Cache(pa, [300, 0, 64, 1, -1, 129], 1, 128, seed=15)
-        c.check(oracle, 8, 5, 1, torch.float32)
-        c = _Cache(pa, [0, 0], 2, 64, seed=16)
-        c.check(oracle, 8, 5, 1)
-        c = _Cache(pa, short, 1, 64, seed=17)
-        c.check(oracle, 3, 5, 1)
-        c = _Cache(pa, [1] * 500 + [6000] + [1] * 300, 2, 64, seed=18)
-        c.check(oracle, 8, 4096, 1, torch.float32)
-
-
-@pytest.mark.parametrize("shares", ["1", "2", "3", "4", "8"])
-@pytest.mark.parametrize("hq,hkv,d", [(14, 2, 128), (16, 4, 64)])
-def test_decode_kv4_rows_shared_by_clusters(pa, oracle, pa_env, hq, hkv, d, shares):
-    """Rows of up to 50 blocks, of one, without a key; more rows than clusters, fewer."""
-    pa_env(PA_DECODE_PATH="persist", PA_DECODE_CLUSTER=shares)
-    lens = [int(x) for x in np.random.default_rng(7).integers(1, 4000, 90)]
-    lens[3:6] = [0, 1, 64]
-    lens[-1] = -7
-    c = _Cache(pa, lens, hkv, d, seed=19)
-    c.check(oracle, hq, 40, 2, torch.float32)
-    c.check(oracle, hq, 40, 2)
-    c = _Cache(pa, [1] * 70 + [3000] + [64] * 80, hkv, d, seed=20)
-    c.check(oracle, hq, 60, 1)
-    c = _Cache(pa, lens[:20], hkv, d, seed=21)
-    c.check(oracle, hq, 40, 2)
+    c = _Cache(pa, short, 1, 64, seed=17)
+    c.check(oracle, 3, 5, 1)
+    c = _Cache(pa, [1] * 500 + [6000] + [1] * 300, 2, 64, seed=18)
+    c.check(oracle, 8, 4096, 1, torch.float32)
 
 
 def test_decode_kv4_long_rows_of_few_sequences(pa, oracle):
@@ -336,7 +318,7 @@ def test_decode_kv4_shared_pages_and_bad_entries(pa, oracle):
     assert torch.equal(o[1:], o2[1:])
 
 
-@pytest.mark.parametrize("path,cluster", [("persist", "1"), ("persist", "4"), ("splitk", "1"), ("cluster", "1"), ("cluster", "3"), ("cluster", "8")])
+@pytest.mark.parametrize("path,cluster", [("persist", "1"), ("cluster", "1"), ("cluster", "3"), ("cluster", "8")])
 def test_decode_kv4_a_wait_that_runs_out_ends_the_kernel(pa, pa_env, path, cluster):
     """Under a limit of one cycle a call ends, with PA_ERR_TIMEOUT or the right result; the calls behind it are right."""
     pa_env(PA_DECODE_PATH=path, PA_DECODE_CLUSTER=cluster, PA_DECODE_STAGES="1")

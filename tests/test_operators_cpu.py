@@ -150,8 +150,8 @@ def test_decode_kv4_refusals(b):
     # a status block of 256 bytes, then two parts of rows per CTA: a number, and (o[128], m, l) of eight heads
     want = 256 + 148 * 2 * (4 + 8 * 130) * 4
     assert b.lib.pa_decode_kv4_workspace_bytes(_changed(good)) == want
-    # no range is longer than 384 blocks: rows of up to 1 + 5 + 3 blocks
-    rows = (148 * 384 // 9 + 4) // 4
+    # no range is longer than 384 blocks, rounded to whole rows of up to 1 + 5 + 3 blocks
+    rows = (148 * (384 - 18) // 9 + 4) // 4
     assert b.lib.pa_decode_kv4_workspace_bytes(_changed(good, batch=rows)) == 256 + 2 * 148 * 2 * (4 + 8 * 130) * 4
     assert status(_changed(good, batch=65535, n_kv_heads=4096, n_q_heads=4096, max_blocks_per_seq=100, head_stride=9216)) == "PA_ERR_SHAPE"
     assert status(_changed(good), ws=0) == status(_changed(good), ws_bytes=want - 1) == "PA_ERR_WORKSPACE"
