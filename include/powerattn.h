@@ -482,10 +482,11 @@ size_t pa_decode_kv4_workspace_bytes(const pa_kv4_params *p);
  * rounded to bf16 for bf16 outputs and held in two bf16 parts for fp32 outputs.
  * workspace: device, 16-byte aligned, >= pa_decode_kv4_workspace_bytes(p); calls that share one must not
  * overlap on the GPU.  A table entry outside [0, n_pages) is clamped into the pool; the sequence's result is
- * then meaningless.  Few rows (sequence and KV head) take one kernel, a thread-block cluster per row; many or long ones
- * two, the first of which gives every warp an equal share of all rows' blocks and the second merges what
- * lies in more than one.  PA_DECODE_PATH=cluster / =persist forces the one or the other, PA_DECODE_CLUSTER=n (1..8)
- * sets the CTAs per row, PA_DECODE_STAGES the blocks that a CTA of a cluster keeps in flight. */
+ * then meaningless.  Few rows (sequence and KV head) take a thread-block cluster each.  Many or long ones are
+ * cut into equal ranges of blocks, one for every warp; one kernel is enqueued, or two where a row may have
+ * parts anywhere, which the second merges.  PA_DECODE_PATH=cluster / =persist forces the one or the other,
+ * PA_DECODE_CLUSTER=n (1..8) sets the CTAs per row, PA_DECODE_STAGES the blocks that a CTA of a cluster keeps
+ * in flight. */
 pa_status pa_decode_kv4(const pa_kv4_params *p, const void *q, const void *kv_pool, const int32_t *block_table,
                         const int32_t *cache_lens, void *o, float *lse, void *workspace, size_t workspace_bytes,
                         void *stream);

@@ -1222,7 +1222,10 @@ extern "C" pa_status pa_decode_kv4(const pa_kv4_params *p, const void *q, const 
     const EnvSwitches env = env_switches();
     const int most = kv4_most_blocks(p);
     const int64_t rows = (int64_t)a.batch * a.Hkv;
-    // Clusters where a row gets all the CTAs it can use, two blocks each at most.
+    // A cluster per row, as many CTAs as run all at once (two per SM), where that is faster than ranges.  Measured with 128 features,
+    // G = 7 (us): a cluster's CTA takes 4 + 0.72 per block, ranges take 14 + 0.26 per block of an SM's share, 9 where they are of
+    // whole rows; with 64 features all of it times 0.6.  Rows of 102 blocks: 144 rows 41 and 43, 192 rows (one CTA each, which
+    // leaves a third of the places empty) 75 and 51; rows of 11 blocks: 192 rows 12.3 and 18.5, 296 rows 12.6 and 13.5.
     int R = 0;
     auto stages_of = [&](int r) {
         // (Each four warps wait for every other block: if stages are used again their number is even, so that a stage is
@@ -1230,17 +1233,18 @@ extern "C" pa_status pa_decode_kv4(const pa_kv4_params *p, const void *q, const 
         const int n = (most + r - 1) / r, room = env.decode_stages ? env.decode_stages : D == 128 ? 6 : 8;
         return n <= room ? n : room < 2 ? 2 : room & ~1;
     };
-    if (env.decode_path != 1 && env.decode_path != 3) {
+    if (env.decode_path != 3) {
         const int64_t fit = (int64_t)dev.sms * 2 / rows;
         R = env.decode_cluster ? env.decode_cluster : fit < kC4MaxCluster ? (int)fit : kC4MaxCluster;
         if (R > most) R = most;
         if (env.decode_path == 2 && R < 1) R = 1;
-        if (env.decode_path != 2 && (R < 1 || (R + 1) * 4 < most)) R = 0;
         for (; R > 1 && !env.decode_cluster; --R) {
             int found = 0;
             if (pa_status s = kv4_resident_clusters(dev.device, D, f32, stages_of(R), R, &found)) return s;
             if (rows <= found) break;
         }
+        const int64_t ranges = (kv4_whole_rows(p) ? 500 : 1000) + 26 * rows * most / kR4Ctas;
+        if (env.decode_path != 2 && (R < 1 || 72 * ((most + R - 1) / R) > ranges)) R = 0;
     }
     if (R > 0) {
         a.R = R;

@@ -203,7 +203,7 @@ def test_decode_kv4(pa, oracle, hq, hkv, d, o_dtype):
 
 
 @pytest.mark.parametrize("env", [{}] + [{"PA_DECODE_PATH": "cluster", "PA_DECODE_CLUSTER": str(r)} for r in range(1, 9)] +
-                         [{"PA_DECODE_PATH": "splitk"}, {"PA_DECODE_PATH": "persist"}] +
+                         [{"PA_DECODE_PATH": "persist"}] +
                          [{"PA_DECODE_PATH": "cluster", "PA_DECODE_STAGES": s, "PA_DECODE_CLUSTER": r} for s in ("1", "2", "5") for r in ("1", "4")])
 @pytest.mark.parametrize("hq,hkv,d", [(14, 2, 128), (4, 1, 64)])
 def test_decode_kv4_forms(pa, oracle, pa_env, hq, hkv, d, env):
@@ -242,6 +242,14 @@ def test_decode_kv4_many_rows(pa, oracle, pa_env):
     c.check(oracle, 3, 5, 1)
     c = _Cache(pa, [1] * 500 + [6000] + [1] * 300, 2, 64, seed=18)
     c.check(oracle, 8, 4096, 1, torch.float32)
+    for hq, hkv, d in ((14, 2, 128), (16, 4, 64)):   # rows of up to 60 blocks, of one, without a key
+        lens = [int(x) for x in np.random.default_rng(7).integers(1, 4000, 90)]
+        lens[3:6] = [0, 1, 64]
+        lens[-1] = -7
+        c = _Cache(pa, lens, hkv, d, seed=19)
+        c.check(oracle, hq, 40, 2)
+        c = _Cache(pa, [1] * 70 + [3000] + [64] * 80, hkv, d, seed=20)
+        c.check(oracle, hq, 60, 1)
 
 
 def test_decode_kv4_long_rows_of_few_sequences(pa, oracle):
