@@ -7,18 +7,17 @@
 //   O = sum_k (p_k s_kj) (u_kj - 8),
 // V's scales folded into the weights: one 16-bit weight per key and group.
 //
-// Logits take fp16 operands: q is bf16, and each head is divided by a power of two so that its largest entry lies in [1, 2) and
-// fits (entries below 2^-14 of it lose bits that are below 2^-24 of it).  Weights are bf16, since V's scales may differ by any
-// factor from key to key and from group to group: rounded once, half a step 2^-8 as the output's own rounding; for fp32
-// outputs they come in two parts.
+// Logits take fp16 operands: q is bf16, and each head is multiplied by a power of two so that its largest entry lies in [2^10, 2^11)
+// and fits (entries below 2^-24 of it lose bits).  Weights are bf16, since V's scales may differ by any factor from key to key
+// and from group to group: rounded once as weights and once times a scale, half a step 2^-8 each, as the output's own
+// rounding; for fp32 outputs they come in two parts.
 //
-// The nibbles become 16-bit numbers without conversions: in fp16 (w & 0x000f000f) | 0x6400 is 1024 + u in both halves and
-// (w & 0x00f000f0) | 0x5400 is 64 + u, in bf16 (w & 0x000f000f) | 0x4300 is 128 + u, each one instruction.  What is too much is
-// taken off by an addition (1024 + u), by the sum that the accumulator starts with (64 + u: -72 sum_i q_i over these
-// features), or by a second product with a constant matrix of -136 (128 + u, a tile of keys at a time, so that nothing large
-// is carried along; fp32 outputs: by an addition).  K rows are stored so that a thread's 16 bytes hold its share of every group; V rows
-// so that the same halfwords of two tokens, put side by side by a byte permutation, are the fragments' key pairs.  Shared
-// memory is read without bank conflicts and without ldmatrix.
+// The nibbles become 16-bit numbers without conversions.  K: w & 0x000f000f is two fp16 subnormals, u 2^-24, and w & 0x00f000f0 is
+// 16 times as much, for which the queries of the former are multiplied by 16; -8 sum_i q_i is what the accumulator starts
+// with.  V: (w & 0x000f000f) | 0x4300 is 128 + u in bf16, and a second product with a constant matrix of -136 takes off what is too
+// much, a tile of keys at a time, so that nothing large is carried along (fp32 outputs: an addition).  K rows are stored so that
+// a thread's 16 bytes hold its share of every group; V rows so that the same halfwords of two tokens, put side by side by a byte
+// permutation, are the fragments' key pairs.  Shared memory is read without bank conflicts and without ldmatrix.
 //
 // Two kernels.  Few rows (sequence and KV head): kv4_cluster_kernel, a thread-block cluster per row, bound by latency.  Many, or
 // long ones: kv4_range_kernel, every warp of the device an equal share of all rows' blocks, bound by instructions and memory.
@@ -78,12 +77,6 @@ __device__ __forceinline__ void mma_b16(float (&d)[4], uint32_t a0, uint32_t a1,
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-__device__ __forceinline__ uint32_t h2_add(uint32_t a, uint32_t b)
-{
-    uint32_t d;
-    asm("add.rn.f16x2 %0, %1, %2;\n" : "=r"(d) : "r"(a), "r"(b));
-    return d;
-}
 // (a & b) | c in one instruction: left to itself the compiler takes two, each with a constant of its own.
 __device__ __forceinline__ uint32_t and_or(uint32_t a, uint32_t b, uint32_t c)
 {
@@ -91,10 +84,9 @@ __device__ __forceinline__ uint32_t and_or(uint32_t a, uint32_t b, uint32_t c)
     asm("lop3.b32 %0, %1, %2, %3, 0xea;\n" : "=r"(d) : "r"(a), "r"(b), "r"(c));
     return d;
 }
-// The lowest nibble of each half of a word as fp16 u - 8, and the one above it as 64 + u (kOver more than u - 8).
-__device__ __forceinline__ uint32_t nib_lo(uint32_t w) { return h2_add(and_or(w, 0x000f000fu, 0x64006400u), 0xe408e408u); }  // - 1032
-__device__ __forceinline__ uint32_t nib_hi(uint32_t w) { return and_or(w, 0x00f000f0u, 0x54005400u); }
-constexpr float kOver = 72.f;
+// The lowest nibble of each half of a word as fp16 u 2^-24, and the one above it as u 2^-20.
+__device__ __forceinline__ uint32_t nib_lo(uint32_t w) { return w & 0x000f000fu; }
+__device__ __forceinline__ uint32_t nib_hi(uint32_t w) { return w & 0x00f000f0u; }
 // The lowest nibble of each half as bf16 128 + u, or u - 8.
 __device__ __forceinline__ uint32_t nib_over(uint32_t w) { return and_or(w, 0x000f000fu, 0x43004300u); }
 constexpr uint32_t kMinus136 = 0xc308c308u;
@@ -168,8 +160,8 @@ template <int D>
 struct Kv4Query {
     static constexpr int NG = D / 32;
     uint32_t f[NG][4];
-    float o0[NG], o1[NG];  // of heads 2t and 2t + 1: -72 times the sum of the features {1, 5, 3, 7} of all t
-    float c0, c1;          // of the same heads: the power of two, the softmax scale, log2 e
+    float o0[NG], o1[NG];  // of heads 2t and 2t + 1: -8 times the sum of the group's features, as the products come (2^-20)
+    float c0, c1;          // of the same heads: the powers of two, the softmax scale, log2 e
     static __device__ __forceinline__ void load(const Kv4Args &a, uint32_t row, int lane, uint4 (&raw)[NG])
     {
         const int g = lane >> 2, t = lane & 3;
@@ -186,23 +178,26 @@ struct Kv4Query {
             for (uint32_t x : {raw[j].x, raw[j].y, raw[j].z, raw[j].w}) top = max(top, max(x & 0x7fffu, (x >> 16) & 0x7fffu));
         top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
         top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-        const uint32_t field = min(max(top >> 7, 27u), 253u);  // (heads below 2^-100 lose bits)
-        const float down = __uint_as_float((254u - field) << 23), up = __uint_as_float(field << 23) * scale_log2;
+        // f is q 2^10 / 2^e with 2^e <= max |q| < 2^(e + 1) (q 2^14 / 2^e where the nibbles come as u 2^-24): products are u q 2^(-10 - e).
+        const uint32_t field = min(max(top >> 7, 27u), 243u);  // e + 127 (heads below 2^-100 lose bits; up to 2^116 they fit)
+        const float down = __uint_as_float((264u - field) << 23), up = __uint_as_float((field + 10u) << 23) * scale_log2;
         c0 = __shfl_sync(0xffffffffu, up, 8 * t);
         c1 = __shfl_sync(0xffffffffu, up, 8 * t + 4);
 #pragma unroll
         for (int j = 0; j < NG; ++j) {
-            f[j][0] = cvt_f16x2(bf16_lo(raw[j].x) * down, bf16_lo(raw[j].z) * down);
+            f[j][0] = cvt_f16x2(bf16_lo(raw[j].x) * (16.f * down), bf16_lo(raw[j].z) * (16.f * down));
             f[j][1] = cvt_f16x2(bf16_hi(raw[j].x) * down, bf16_hi(raw[j].z) * down);
-            f[j][2] = cvt_f16x2(bf16_lo(raw[j].y) * down, bf16_lo(raw[j].w) * down);
+            f[j][2] = cvt_f16x2(bf16_lo(raw[j].y) * (16.f * down), bf16_lo(raw[j].w) * (16.f * down));
             f[j][3] = cvt_f16x2(bf16_hi(raw[j].y) * down, bf16_hi(raw[j].w) * down);
-            const float2 x = __half22float2(*reinterpret_cast<const __half2 *>(&f[j][1]));
-            const float2 y = __half22float2(*reinterpret_cast<const __half2 *>(&f[j][3]));
-            float sum = (x.x + x.y) + (y.x + y.y);
+            float2 x[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] = __half22float2(*reinterpret_cast<const __half2 *>(&f[j][i]));
+            float sum = ((x[0].x + x[0].y) + (x[2].x + x[2].y)) * 0.0625f + ((x[1].x + x[1].y) + (x[3].x + x[3].y));
             sum += __shfl_xor_sync(0xffffffffu, sum, 1);
             sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-            o0[j] = -kOver * __shfl_sync(0xffffffffu, sum, 8 * t);
-            o1[j] = -kOver * __shfl_sync(0xffffffffu, sum, 8 * t + 4);
+            sum *= -8.f * 0x1p-20f;
+            o0[j] = __shfl_sync(0xffffffffu, sum, 8 * t);
+            o1[j] = __shfl_sync(0xffffffffu, sum, 8 * t + 4);
         }
     }
 };
