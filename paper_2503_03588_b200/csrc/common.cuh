@@ -38,7 +38,7 @@ enum DeviceOnce : int {
     ONCE_PREFILL_ATTR = 0,  // (40: order of the units, head_dim, slots, output type)
     ONCE_DECODE_ATTR = ONCE_PREFILL_ATTR + 40,
     ONCE_BACKWARD_ATTR, ONCE_BACKWARD_ATTR_64, ONCE_BACKWARD_TC_ATTR, ONCE_BACKWARD_TC_ATTR_64,
-    ONCE_KV4_ATTR,
+    ONCE_KV4_ATTR, ONCE_ROPE_ATTR,
     ONCE_COUNT
 };
 std::mutex &device_once_mutex();

@@ -210,18 +210,32 @@ __global__ void __launch_bounds__(kRopeThreads) rope_few_kernel(const RopeArgs a
     if (in) write_bf16<kPairs>(turned(v, r, factors(w, load_angles(a, p, pos)), p.rotated), out + p.a, out + p.b);
 }
 
-// Forward.  Warps stride over the tokens, 2 x 512 / D heads at a time; the next ones, of the next token too, are on their way while
-// these are worked on.  A lane has sixteen features here, two times eight numbers as above: half the instructions a head, of
-// which there were too many with eight (32K tokens, 28 / 4 heads: 100 us).
+__device__ __forceinline__ void copy16(uint32_t dst, const void *src)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;\n" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;\n" ::: "memory"); }
+template <int kLeft>
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;\n" ::"n"(kLeft) : "memory"); }
+
+// Forward.  Warps stride over the tokens, 512 / D heads at a time, queries, then keys.  A lane has sixteen features here, two times
+// eight numbers as above: half the instructions a head.  What a lane will need of the next kRopeAhead turns is on its way to
+// places of its own in shared memory (nobody else reads them, so there is nothing to wait for but its own copies).
+constexpr int kRopeAhead = 8;
+constexpr int kRopeTurn = 32 * 32;  // bytes of a turn: 32 of a lane
+
 template <int D, bool kPairs>
 __global__ void __launch_bounds__(kBackThreads, 2) rope_kernel(const RopeArgs a)
 {
-    constexpr int kLanes = D / 16, kHeads = 32 / kLanes, kBatch = 2;
+    constexpr int kLanes = D / 16, kHeads = 32 / kLanes;
+    extern __shared__ __align__(16) uint8_t rope_smem[];
     pdl_launch_next();
     const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, l = lane % kLanes, mine = lane / kLanes;
     const bool rotated = 8 * l < a.half;
     const int pa = !kPairs && rotated ? 8 * l : 16 * l, pb = !kPairs && rotated ? a.half + 8 * l : 16 * l + 8;
+    const uint8_t *ring = rope_smem + wid * (kRopeAhead * kRopeTurn) + lane * 16;
     const int64_t step = (int64_t)gridDim.x * kBackWarps;
+    const int turns_q = (a.Hq + kHeads - 1) / kHeads, turns = turns_q + (a.Hkv + kHeads - 1) / kHeads;
     pdl_wait();
     auto position = [&](int64_t token) {  // -1: none
         const int32_t pos = token < a.tokens ? a.positions[token] : -1;
@@ -231,30 +245,48 @@ __global__ void __launch_bounds__(kBackThreads, 2) rope_kernel(const RopeArgs a)
         const int64_t b = a.seq >= a.tokens ? 0 : token / a.seq;
         return b * s.batch + (token - b * a.seq) * s.seq + mine * s.head;
     };
-    uint4 ra[kBatch], rb[kBatch];
-    auto load = [&](const __nv_bfloat16 *x, int64_t x_step, int heads) {  // (heads from this lane's first one on)
-#pragma unroll
-        for (int y = 0; y < kBatch; ++y) {
-            ra[y] = rb[y] = make_uint4(0u, 0u, 0u, 0u);
-            if (y * kHeads < heads) {
-                ra[y] = *reinterpret_cast<const uint4 *>(x + pa);
-                rb[y] = *reinterpret_cast<const uint4 *>(x + pb);
+    // What is fetched next.
+    int64_t f_token = (int64_t)blockIdx.x * kBackWarps + wid;
+    int f_turn = 0, f_left = 0, f_slot = 0;  // heads left from this lane's one on
+    const __nv_bfloat16 *x = nullptr;
+    int64_t x_step = 0;
+    auto fetch = [&] {
+        if (f_token < a.tokens) {
+            if (f_turn == 0) {
+                x = a.q + place(f_token, a.sq);
+                x_step = kHeads * a.sq.head;
+                f_left = a.Hq - mine;
+            } else if (f_turn == turns_q) {
+                x = a.k + place(f_token, a.sk);
+                x_step = kHeads * a.sk.head;
+                f_left = a.Hkv - mine;
+            }
+            if (f_left > 0) {
+                const uint32_t at = ptx::smem_u32(ring) + f_slot * kRopeTurn;
+                copy16(at, x + pa);
+                copy16(at + 512, x + pb);
             }
             x += x_step;
+            f_left -= kHeads;
+            if (++f_turn == turns) {
+                f_turn = 0;
+                f_token += step;
+            }
         }
+        copies_commit();
+        f_slot = (f_slot + 1) % kRopeAhead;
     };
+    for (int y = 0; y < kRopeAhead; ++y) fetch();
+    int slot = 0;
     int64_t token = (int64_t)blockIdx.x * kBackWarps + wid;
-    if (token >= a.tokens) return;
     int32_t pos = position(token), pos_next = position(token + step);
-    load(a.q + place(token, a.sq), kHeads * a.sq.head, a.Hq - mine);
     for (; token < a.tokens; token += step) {
         const int32_t pos_after = position(token + 2 * step);
 #pragma unroll 1
         for (int which = 0; which < 2; ++which) {
             const int H = which ? a.Hkv : a.Hq;
-            const pa_strides &sx = which ? a.sk : a.sq, &so = which ? a.sko : a.sqo;
-            const int64_t x_step = kHeads * sx.head, out_step = kHeads * so.head;
-            const __nv_bfloat16 *x = (which ? a.k : a.q) + place(token, sx);
+            const pa_strides &so = which ? a.sko : a.sqo;
+            const int64_t out_step = kHeads * so.head;
             __nv_bfloat16 *out = (which ? a.k_out : a.q_out) + place(token, so);
             Factors f[2];
             {
@@ -278,46 +310,39 @@ __global__ void __launch_bounds__(kBackThreads, 2) rope_kernel(const RopeArgs a)
                     f[e] = factors(load_weights<kPairs>(w, a.w_f32, p), t);
                 }
             }
-            for (int h = 0; h < H; h += kBatch * kHeads) {
-                uint4 va[kBatch], vb[kBatch];
+            for (int h = mine; h - mine < H; h += kHeads) {
+                copies_wait<kRopeAhead - 1>();
+                const uint4 va = *reinterpret_cast<const uint4 *>(ring + slot * kRopeTurn);
+                const uint4 vb = *reinterpret_cast<const uint4 *>(ring + slot * kRopeTurn + 512);
+                slot = (slot + 1) % kRopeAhead;
+                const Eight v[2] = {from_bf16<kPairs>(make_uint2(va.x, va.y), make_uint2(vb.x, vb.y)),
+                                    from_bf16<kPairs>(make_uint2(va.z, va.w), make_uint2(vb.z, vb.w))};
+                uint64_t sq[2] = {0, 0};
 #pragma unroll
-                for (int y = 0; y < kBatch; ++y) {
-                    va[y] = ra[y];
-                    vb[y] = rb[y];
+                for (int i = 0; i < 4; ++i) {
+                    sq[0] = fma_f32x2(v[0].v[i], v[0].v[i], sq[0]);
+                    sq[1] = fma_f32x2(v[1].v[i], v[1].v[i], sq[1]);
                 }
-                x += kBatch * x_step;
-                if (h + kBatch * kHeads < H) load(x, x_step, H - mine - (h + kBatch * kHeads));
-                else if (which == 0) load(a.k + place(token, a.sk), kHeads * a.sk.head, a.Hkv - mine);
-                else if (token + step < a.tokens) load(a.q + place(token + step, a.sq), kHeads * a.sq.head, a.Hq - mine);
+                const uint64_t r = both(rsqrtf(sum_lanes<kLanes>(sum_pairs(add_f32x2(sq[0], sq[1]))) * (1.0f / D) + a.eps));
+                fetch();  // (behind the last use of what was in its place)
+                float o[2][8];
 #pragma unroll
-                for (int y = 0; y < kBatch; ++y) {
-                    Eight v[2] = {from_bf16<kPairs>(make_uint2(va[y].x, va[y].y), make_uint2(vb[y].x, vb[y].y)),
-                                  from_bf16<kPairs>(make_uint2(va[y].z, va[y].w), make_uint2(vb[y].z, vb[y].w))};
-                    uint64_t sq[2] = {0, 0};
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        sq[0] = fma_f32x2(v[0].v[i], v[0].v[i], sq[0]);
-                        sq[1] = fma_f32x2(v[1].v[i], v[1].v[i], sq[1]);
-                    }
-                    const uint64_t r = both(rsqrtf(sum_lanes<kLanes>(sum_pairs(add_f32x2(sq[0], sq[1]))) * (1.0f / D) + a.eps));
-                    float o[2][8];
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) pieces<kPairs>(turned(v[e], r, f[e], rotated), o[e]);
-                    if (pos >= 0 && h + y * kHeads + mine < H) {
-                        auto four = [&](int i) {
-                            return make_uint4(ptx::cvt_bf16x2(o[0][i], o[0][i + 1]), ptx::cvt_bf16x2(o[0][i + 2], o[0][i + 3]),
-                                              ptx::cvt_bf16x2(o[1][i], o[1][i + 1]), ptx::cvt_bf16x2(o[1][i + 2], o[1][i + 3]));
-                        };
-                        *reinterpret_cast<uint4 *>(out + pa) = four(0);
-                        *reinterpret_cast<uint4 *>(out + pb) = four(4);
-                    }
-                    out += out_step;
+                for (int e = 0; e < 2; ++e) pieces<kPairs>(turned(v[e], r, f[e], rotated), o[e]);
+                if (pos >= 0 && h < H) {
+                    auto four = [&](int i) {
+                        return make_uint4(ptx::cvt_bf16x2(o[0][i], o[0][i + 1]), ptx::cvt_bf16x2(o[0][i + 2], o[0][i + 3]),
+                                          ptx::cvt_bf16x2(o[1][i], o[1][i + 1]), ptx::cvt_bf16x2(o[1][i + 2], o[1][i + 3]));
+                    };
+                    *reinterpret_cast<uint4 *>(out + pa) = four(0);
+                    *reinterpret_cast<uint4 *>(out + pb) = four(4);
                 }
+                out += out_step;
             }
         }
         pos = pos_next;
         pos_next = pos_after;
     }
+    copies_wait<0>();
 }
 
 // Backward.  Warps stride over the tokens and keep the weights' gradients in registers; at the end a CTA adds its warps' up, in
@@ -561,11 +586,21 @@ extern "C" pa_status pa_qk_norm_rope(const pa_rope_params *p, const void *q, con
     static void (*const many[2][2])(const RopeArgs) = {{rope_kernel<64, false>, rope_kernel<64, true>},
                                                        {rope_kernel<128, false>, rope_kernel<128, true>}};
     const int64_t warps = a.tokens * a.chunks;
+    DeviceInfo dev;
+    if (pa_status s = current_sm100_device(&dev)) return s;
+    if (pa_status s = device_once(dev.device, ONCE_ROPE_ATTR, [] {
+            cudaError_t e = cudaSuccess;
+            for (int i = 0; i < 4; ++i)
+                e = first_error(e, cudaFuncSetAttribute(many[i >> 1][i & 1], cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                                        kBackWarps * kRopeAhead * kRopeTurn));
+            return e;
+        }))
+        return s;
     if (warps <= kRopeFewWarps)
         PA_CUDA_OK(launch_pdl(few[p->head_dim == 128][p->interleaved != 0], dim3((unsigned)((warps + kRopeWarps - 1) / kRopeWarps)),
                               kRopeThreads, 0, st, a));
     else
-        PA_CUDA_OK(launch_pdl(many[p->head_dim == 128][p->interleaved != 0], dim3((unsigned)token_ctas(p)), kBackThreads, 0, st, a));
+        PA_CUDA_OK(launch_pdl(many[p->head_dim == 128][p->interleaved != 0], dim3((unsigned)token_ctas(p)), kBackThreads, kBackWarps * kRopeAhead * kRopeTurn, st, a));
     return PA_OK;
 }
 
