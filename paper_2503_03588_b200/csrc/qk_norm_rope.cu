@@ -470,22 +470,28 @@ __global__ void __launch_bounds__(kBackThreads, 2) rope_backward_kernel(const Ro
     }
 }
 
-// Sums over the CTAs of rope_backward_kernel: 32 columns a CTA, 32 rows at a time.
-__global__ void __launch_bounds__(1024) rope_weights_kernel(const float *parts, int n, int D, float *dq_weight, float *dk_weight)
+// Sums over the CTAs of rope_backward_kernel: 8 columns a CTA, a sector of each of 128 rows at a time, added up in a fixed order.
+constexpr int kSumThreads = 1024;
+__global__ void __launch_bounds__(kSumThreads) rope_weights_kernel(const float *parts, int n, int D, float *dq_weight, float *dk_weight)
 {
-    __shared__ float sums[32][33];
+    __shared__ float sums[kSumThreads / 32][8];
     pdl_launch_next();
-    const int x = threadIdx.x & 31, y = threadIdx.x >> 5, f = blockIdx.x * 32 + x;
+    const int x = threadIdx.x & 7, y = threadIdx.x >> 3, f = blockIdx.x * 8 + x;
     pdl_wait();
     float t = 0.f;
-    for (int i = y; i < n; i += 32) t += parts[(int64_t)i * 2 * D + f];
-    sums[y][x] = t;
+#pragma unroll 4
+    for (int i = y; i < n; i += kSumThreads / 8) t += parts[(int64_t)i * 2 * D + f];
+    t += __shfl_xor_sync(0xffffffffu, t, 8);
+    t += __shfl_xor_sync(0xffffffffu, t, 16);
+    if ((threadIdx.x & 31) < 8) sums[threadIdx.x >> 5][x] = t;
     __syncthreads();
-    if (y == 0) {
+    if (threadIdx.x < 32) {  // lane: column x, rows lane / 8, lane / 8 + 4, ...
         t = 0.f;
 #pragma unroll
-        for (int i = 0; i < 32; ++i) t += sums[i][x];
-        (f < D ? dq_weight : dk_weight)[f % D] = t;
+        for (int i = 0; i < kSumThreads / 32; i += 4) t += sums[i + (threadIdx.x >> 3)][x];
+        t += __shfl_xor_sync(0xffffffffu, t, 8);
+        t += __shfl_xor_sync(0xffffffffu, t, 16);
+        if (threadIdx.x < 8) (f < D ? dq_weight : dk_weight)[f % D] = t;
     }
 }
 
@@ -562,7 +568,10 @@ static int64_t token_ctas(const pa_rope_params *p)
     const int64_t need = ((int64_t)p->batch * p->seq_len + kBackWarps - 1) / kBackWarps;
     return need < kRopeCtas ? need : kRopeCtas;
 }
-constexpr int64_t kRopeFewWarps = 148 * 64;  // warps that run all at once
+// Up to this many warps of one piece each, else the persistent ones that ring.  Measured (us, one piece a warp and persistent):
+// 28 and 4 heads of 128 features, 600 tokens 4.6 and 6.5, 1200 tokens 7.5 and 7.2, 2500 tokens 14.0 and 10.3; 16 and 4 heads of
+// 64, 1200 tokens 3.4 and 4.5, 2500 tokens 5.5 and 6.1, 5000 tokens 9.4 and 8.7.
+constexpr int64_t kRopeFewWarps = 148 * 112;
 
 }  // namespace pa
 
@@ -600,7 +609,8 @@ extern "C" pa_status pa_qk_norm_rope(const pa_rope_params *p, const void *q, con
         PA_CUDA_OK(launch_pdl(few[p->head_dim == 128][p->interleaved != 0], dim3((unsigned)((warps + kRopeWarps - 1) / kRopeWarps)),
                               kRopeThreads, 0, st, a));
     else
-        PA_CUDA_OK(launch_pdl(many[p->head_dim == 128][p->interleaved != 0], dim3((unsigned)token_ctas(p)), kBackThreads, kBackWarps * kRopeAhead * kRopeTurn, st, a));
+        PA_CUDA_OK(launch_pdl(many[p->head_dim == 128][p->interleaved != 0], dim3((unsigned)token_ctas(p)), kBackThreads,
+                              kBackWarps * kRopeAhead * kRopeTurn, st, a));
     return PA_OK;
 }
 
@@ -643,7 +653,7 @@ extern "C" pa_status pa_qk_norm_rope_backward(const pa_rope_params *p, const voi
                                                               {rope_backward_kernel<128, true, bf16>, rope_backward_kernel<128, true, float>}}};
     auto launch = [&](auto kernel) { return launch_pdl(kernel, dim3((unsigned)ctas), kBackThreads, 0, st, a); };
     PA_CUDA_OK(launch(kernels[p->head_dim == 128][p->interleaved != 0][d_dtype == PA_F32]));
-    PA_CUDA_OK(launch_pdl(rope_weights_kernel, dim3((unsigned)(2 * p->head_dim / 32)), 1024, 0, st,
+    PA_CUDA_OK(launch_pdl(rope_weights_kernel, dim3((unsigned)(2 * p->head_dim / 8)), kSumThreads, 0, st,
                           static_cast<const float *>(a.parts), (int)ctas, (int)p->head_dim, dq_weight, dk_weight));
     return PA_OK;
 }
