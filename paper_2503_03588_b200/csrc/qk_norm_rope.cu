@@ -84,20 +84,34 @@ __device__ __forceinline__ void write_bf16(const Eight &e, __nv_bfloat16 *a, __n
 }
 __device__ __forceinline__ uint2 ld8(const void *p) { return *reinterpret_cast<const uint2 *>(p); }
 
-// Where a lane's pieces stand in a head, and the first of its four angles.  Rotated features in halves: the lane's first numbers
-// in piece a, their partners half a rotated part further on; else eight neighbours.
+// Where a lane's two pieces of four features stand in a head, which of its pairs [0] and [1] are rotated, and the first of their
+// angles.  Neighbours' pieces are neighbours, so that a load or a store of a warp fills its sectors.
 struct Pieces {
-    int a, b, angle;
-    bool rotated;
+    int a, b, angle[2];
+    bool turn[2];
 };
-template <bool kPairs>
-__device__ __forceinline__ Pieces pieces_of(int l, int half)
+// Lane l of kLanes: pieces of kWide features, of them the four from 4 part on.  Rotated features in halves: the lane's first numbers
+// in piece a, their partners half a rotated part further on; the rest of the head is shared out behind them.  In neighbouring
+// pairs: one piece of each half of the head.
+template <int D, bool kPairs, int kWide>
+__device__ __forceinline__ Pieces pieces_of(int l, int half, int part = 0)
 {
     Pieces p;
-    p.angle = 4 * l;
-    p.rotated = 4 * l < half;
-    p.a = !kPairs && p.rotated ? 4 * l : 8 * l;
-    p.b = !kPairs && p.rotated ? half + 4 * l : 8 * l + 4;
+    if (kPairs) {
+        p.a = kWide * l + 4 * part;
+        p.b = D / 2 + p.a;
+        p.turn[0] = p.a < 2 * half;
+        p.turn[1] = p.b < 2 * half;
+        p.angle[0] = p.a / 2;
+        p.angle[1] = p.b / 2;
+    } else {
+        const bool turn = kWide * l < half;
+        p.a = (turn ? 0 : half) + kWide * l + 4 * part;
+        p.b = p.a + (turn ? half : D / 2 - half);
+        p.turn[0] = p.turn[1] = turn;
+        p.angle[0] = p.a;
+        p.angle[1] = p.a + 2;
+    }
     return p;
 }
 template <bool kPairs, typename T>
@@ -119,15 +133,26 @@ __device__ __forceinline__ Eight load_weights(const void *w, bool f32, const Pie
 struct Angles {
     uint64_t c[2], s[2];
 };
+template <bool kPairs>
 __device__ __forceinline__ Angles load_angles(const RopeArgs &a, const Pieces &p, int32_t pos)
 {
-    float4 u = make_float4(1.f, 1.f, 1.f, 1.f), v = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (p.rotated) {
-        const float *row = a.cos_sin + (int64_t)pos * (2 * a.half) + p.angle;
-        u = *reinterpret_cast<const float4 *>(row);
-        v = *reinterpret_cast<const float4 *>(row + a.half);
+    Angles t = {{both(1.f), both(1.f)}, {0, 0}};
+    const float *row = a.cos_sin + (int64_t)pos * (2 * a.half);
+    if (kPairs) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            if (p.turn[i]) {
+                const float2 u = *reinterpret_cast<const float2 *>(row + p.angle[i]);
+                const float2 v = *reinterpret_cast<const float2 *>(row + a.half + p.angle[i]);
+                t.c[i] = pack_f32x2(u.x, u.y);
+                t.s[i] = pack_f32x2(v.x, v.y);
+            }
+    } else if (p.turn[0]) {
+        const float4 u = *reinterpret_cast<const float4 *>(row + p.angle[0]);
+        const float4 v = *reinterpret_cast<const float4 *>(row + a.half + p.angle[0]);
+        t = {{pack_f32x2(u.x, u.y), pack_f32x2(u.z, u.w)}, {pack_f32x2(v.x, v.y), pack_f32x2(v.z, v.w)}};
     }
-    return {{pack_f32x2(u.x, u.y), pack_f32x2(u.z, u.w)}, {pack_f32x2(v.x, v.y), pack_f32x2(v.z, v.w)}};
+    return t;
 }
 template <int kLanes>
 __device__ __forceinline__ float sum_lanes(float x)
@@ -162,13 +187,13 @@ __device__ __forceinline__ Factors factors(const Eight &w, const Angles &t)
     return f;
 }
 // Numbers times r, multiplied and rotated.
-__device__ __forceinline__ Eight turned(const Eight &v, uint64_t r, const Factors &k, bool rotated)
+__device__ __forceinline__ Eight turned(const Eight &v, uint64_t r, const Factors &k, const Pieces &p)
 {
     Eight o;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         const uint64_t f = mul_f32x2(v.v[i], r), g = mul_f32x2(v.v[2 + i], r);
-        if (rotated) {
+        if (p.turn[i]) {
             o.v[i] = fma_f32x2(f, k.fc[i], mul_f32x2(g, k.ss[i]));
             o.v[2 + i] = fma_f32x2(g, k.sc[i], mul_f32x2(f, k.fs[i]));
         } else {
@@ -186,7 +211,7 @@ __global__ void __launch_bounds__(kRopeThreads) rope_few_kernel(const RopeArgs a
     constexpr int kLanes = D / 8, kHeads = 32 / kLanes;
     pdl_launch_next();
     const int lane = threadIdx.x & 31, l = lane % kLanes, mine = lane / kLanes;
-    const Pieces p = pieces_of<kPairs>(l, a.half);
+    const Pieces p = pieces_of<D, kPairs, 4>(l, a.half);
     const int64_t item = (int64_t)blockIdx.x * kRopeWarps + (threadIdx.x >> 5), token = item / a.chunks;
     const int h0 = (int)(item - token * a.chunks) * kHeads + mine, q_chunks = (a.Hq + kHeads - 1) / kHeads * kHeads;
     const bool is_k = h0 - mine >= q_chunks;
@@ -207,7 +232,7 @@ __global__ void __launch_bounds__(kRopeThreads) rope_few_kernel(const RopeArgs a
 #pragma unroll
     for (int i = 0; i < 4; ++i) sq = fma_f32x2(v.v[i], v.v[i], sq);
     const uint64_t r = both(rsqrtf(sum_lanes<kLanes>(sum_pairs(sq)) * (1.0f / D) + a.eps));
-    if (in) write_bf16<kPairs>(turned(v, r, factors(w, load_angles(a, p, pos)), p.rotated), out + p.a, out + p.b);
+    if (in) write_bf16<kPairs>(turned(v, r, factors(w, load_angles<kPairs>(a, p, pos)), p), out + p.a, out + p.b);
 }
 
 __device__ __forceinline__ void copy16(uint32_t dst, const void *src)
@@ -231,8 +256,7 @@ __global__ void __launch_bounds__(kBackThreads, 2) rope_kernel(const RopeArgs a)
     extern __shared__ __align__(16) uint8_t rope_smem[];
     pdl_launch_next();
     const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, l = lane % kLanes, mine = lane / kLanes;
-    const bool rotated = 8 * l < a.half;
-    const int pa = !kPairs && rotated ? 8 * l : 16 * l, pb = !kPairs && rotated ? a.half + 8 * l : 16 * l + 8;
+    const Pieces p[2] = {pieces_of<D, kPairs, 8>(l, a.half, 0), pieces_of<D, kPairs, 8>(l, a.half, 1)};
     const uint8_t *ring = rope_smem + wid * (kRopeAhead * kRopeTurn) + lane * 16;
     const int64_t step = (int64_t)gridDim.x * kBackWarps;
     const int turns_q = (a.Hq + kHeads - 1) / kHeads, turns = turns_q + (a.Hkv + kHeads - 1) / kHeads;
@@ -263,8 +287,8 @@ __global__ void __launch_bounds__(kBackThreads, 2) rope_kernel(const RopeArgs a)
             }
             if (f_left > 0) {
                 const uint32_t at = ptx::smem_u32(ring) + f_slot * kRopeTurn;
-                copy16(at, x + pa);
-                copy16(at + 512, x + pb);
+                copy16(at, x + p[0].a);
+                copy16(at + 512, x + p[0].b);
             }
             x += x_step;
             f_left -= kHeads;
@@ -289,27 +313,9 @@ __global__ void __launch_bounds__(kBackThreads, 2) rope_kernel(const RopeArgs a)
             const int64_t out_step = kHeads * so.head;
             __nv_bfloat16 *out = (which ? a.k_out : a.q_out) + place(token, so);
             Factors f[2];
-            {
-                float c[8] = {1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f}, s[8] = {};
-                if (rotated) {
-                    const float *row = a.cos_sin + (int64_t)(pos < 0 ? 0 : pos) * (2 * a.half) + 8 * l;
 #pragma unroll
-                    for (int i = 0; i < 8; i += 4) {
-                        const float4 u = *reinterpret_cast<const float4 *>(row + i), v = *reinterpret_cast<const float4 *>(row + a.half + i);
-                        c[i] = u.x; c[i + 1] = u.y; c[i + 2] = u.z; c[i + 3] = u.w;
-                        s[i] = v.x; s[i + 1] = v.y; s[i + 2] = v.z; s[i + 3] = v.w;
-                    }
-                }
-                const void *w = which ? a.k_weight : a.q_weight;
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const Pieces p = {pa + 4 * e, pb + 4 * e, 0, rotated};
-                    const int i = kPairs ? 2 * e : 4 * e, j = kPairs ? 4 + 2 * e : 4 * e + 2;
-                    const Angles t = {{pack_f32x2(c[i], c[i + 1]), pack_f32x2(c[j], c[j + 1])},
-                                      {pack_f32x2(s[i], s[i + 1]), pack_f32x2(s[j], s[j + 1])}};
-                    f[e] = factors(load_weights<kPairs>(w, a.w_f32, p), t);
-                }
-            }
+            for (int e = 0; e < 2; ++e)
+                f[e] = factors(load_weights<kPairs>(which ? a.k_weight : a.q_weight, a.w_f32, p[e]), load_angles<kPairs>(a, p[e], pos < 0 ? 0 : pos));
             for (int h = mine; h - mine < H; h += kHeads) {
                 copies_wait<kRopeAhead - 1>();
                 const uint4 va = *reinterpret_cast<const uint4 *>(ring + slot * kRopeTurn);
@@ -327,14 +333,14 @@ __global__ void __launch_bounds__(kBackThreads, 2) rope_kernel(const RopeArgs a)
                 fetch();  // (behind the last use of what was in its place)
                 float o[2][8];
 #pragma unroll
-                for (int e = 0; e < 2; ++e) pieces<kPairs>(turned(v[e], r, f[e], rotated), o[e]);
+                for (int e = 0; e < 2; ++e) pieces<kPairs>(turned(v[e], r, f[e], p[e]), o[e]);
                 if (pos >= 0 && h < H) {
                     auto four = [&](int i) {
                         return make_uint4(ptx::cvt_bf16x2(o[0][i], o[0][i + 1]), ptx::cvt_bf16x2(o[0][i + 2], o[0][i + 3]),
                                           ptx::cvt_bf16x2(o[1][i], o[1][i + 1]), ptx::cvt_bf16x2(o[1][i + 2], o[1][i + 3]));
                     };
-                    *reinterpret_cast<uint4 *>(out + pa) = four(0);
-                    *reinterpret_cast<uint4 *>(out + pb) = four(4);
+                    *reinterpret_cast<uint4 *>(out + p[0].a) = four(0);
+                    *reinterpret_cast<uint4 *>(out + p[0].b) = four(4);
                 }
                 out += out_step;
             }
@@ -354,7 +360,7 @@ __global__ void __launch_bounds__(kBackThreads, 2) rope_backward_kernel(const Ro
     __shared__ float sums[kBackWarps * kHeads][2][D];
     pdl_launch_next();
     const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, l = lane % kLanes, mine = lane / kLanes;
-    const Pieces p = pieces_of<kPairs>(l, a.half);
+    const Pieces p = pieces_of<D, kPairs, 4>(l, a.half);
     Eight dw[2] = {};
     pdl_wait();
     for (int64_t token = (int64_t)blockIdx.x * kBackWarps + wid; token < a.tokens; token += (int64_t)gridDim.x * kBackWarps) {
@@ -398,7 +404,7 @@ __global__ void __launch_bounds__(kBackThreads, 2) rope_backward_kernel(const Ro
             load(0);
             const Eight w = load_weights<kPairs>(which ? a.k_weight : a.q_weight, a.w_f32, p);
             if (!looked_up) {
-                t = load_angles(a, p, there ? pos : 0);
+                t = load_angles<kPairs>(a, p, there ? pos : 0);
                 looked_up = true;
             }
             for (int h = 0; h < H; h += kBatch * kHeads) {
@@ -417,14 +423,13 @@ __global__ void __launch_bounds__(kBackThreads, 2) rope_backward_kernel(const Ro
 #pragma unroll
                 for (int y = 0; y < kBatch; ++y) {
                     const bool in = h + y * kHeads + mine < H;
-                    if (p.rotated) {  // back by the angle
 #pragma unroll
-                        for (int i = 0; i < 2; ++i) {
+                    for (int i = 0; i < 2; ++i)
+                        if (p.turn[i]) {  // back by the angle
                             const uint64_t f = g[y].v[i], s = g[y].v[2 + i];
                             g[y].v[i] = fma_f32x2(f, t.c[i], mul_f32x2(s, t.s[i]));
                             g[y].v[2 + i] = fma_f32x2(s, t.c[i], negative(mul_f32x2(f, t.s[i])));
                         }
-                    }
                     // dx = r (h - x^ mean(h x^)), h = g w, x^ = x r;  dw = sum g x^
                     Eight gw;
                     uint64_t sq = 0, along = 0;
