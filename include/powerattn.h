@@ -378,7 +378,8 @@ size_t pa_build_block_tables_workspace_bytes(const pa_table_params *p);
  * [free_capacity]; free_count, free_left int32 [1]; block_table int32 [batch, max_blocks_per_seq], read
  * and written; cu_seqlens int32 [batch + 1]; slot_map int64 [max_tokens]; positions int32 [max_tokens].
  * lens_out may be cache_lens and free_left may be free_count; no other two may overlap.  One kernel is
- * enqueued, or two: for more than 1024 sequences, or more than 1024 tokens with results in place.  Calls that share a workspace must not overlap on the GPU.
+ * enqueued, or two: for more than 1024 sequences, or more than 1024 tokens with results in place.  Calls
+ * that share a workspace must not overlap on the GPU.
  * Errors: PA_ERR_INVALID_ARG, PA_ERR_SHAPE, PA_ERR_ALIGNMENT, PA_ERR_WORKSPACE, PA_ERR_CUDA. */
 pa_status pa_build_block_tables(const pa_table_params *p, const int32_t *new_lens, const int32_t *cache_lens,
                                 const int32_t *free_pages, const int32_t *free_count, int32_t *block_table,
