@@ -10,6 +10,7 @@
 
 #include "common.cuh"
 #include "kv4.cuh"
+#include "sm100_ptx.cuh"
 
 namespace pa {
 
@@ -48,7 +49,8 @@ __device__ __forceinline__ Kv4Place place_of(const Kv4CacheArgs &a)
 template <int D>
 __device__ __forceinline__ uint8_t *half_record(const Kv4CacheArgs &a, const Kv4Place &p, int64_t slot)
 {
-    return a.pool + (slot / kKv4Page) * a.page_stride + p.head * a.head_stride + (p.is_v ? Kv4Record<D>::kHalf : 0);
+    return a.pool + (int64_t)(uint32_t)((uint64_t)slot / kKv4Page) * a.page_stride + p.head * a.head_stride +
+           (p.is_v ? Kv4Record<D>::kHalf : 0);
 }
 // Byte in its row at which the nibbles of features 4 h .. 4 h + 3 stand, a halfword.  (K: of features 8 c .. 8 c + 7, a word at the
 // place of h = 2 c.)
@@ -96,7 +98,6 @@ __global__ void __launch_bounds__(kKv4Threads) kv4_append_kernel(const Kv4CacheA
         two = max_magnitude(two, __shfl_xor_sync(0xffffffffu, two, 1));
         two = max_magnitude(two, __shfl_xor_sync(0xffffffffu, two, 2));
         const uint32_t top = max(two & 0xffffu, two >> 16);  // (patterns without sign are ordered as integers, NaN on top)
-        if (slot[y] < 0 || slot[y] >= a.n_slots) continue;
         // s = amax / 7 in bf16.  A quotient by 7 is never near enough to the middle of two bf16 numbers for the fp32 product to
         // round differently (it is 1/14 of a step away at least).
         const float amax = __uint_as_float(top << 16);
@@ -116,25 +117,29 @@ __global__ void __launch_bounds__(kKv4Threads) kv4_append_kernel(const Kv4CacheA
             word = (word * 16u + n1) * 16u + n0;
         }
         word -= kPattern * kAll;
-        const int place = (int)(slot[y] % kKv4Page);
-        uint8_t *half = half_record<D>(a, p, slot[y]), *row = half + place * R::kRow;
-        if (p.is_v) {
-            *reinterpret_cast<uint16_t *>(row + v_byte<D>(2 * p.c, place)) = (uint16_t)word;
-            *reinterpret_cast<uint16_t *>(row + v_byte<D>(2 * p.c + 1, place)) = (uint16_t)(word >> 16);
-        } else {
-            *reinterpret_cast<uint32_t *>(row + k_byte<D>(2 * p.c)) = word;
-        }
+        // V: its two halfwords belong into two chunks.  The thread with the same features of the next group has their neighbours,
+        // and each of the two takes a chunk.
+        const uint32_t other = __shfl_xor_sync(0xffffffffu, word, 4);
+        if (p.is_v) word = __byte_perm(word, other, p.c & 4 ? 0x3276 : 0x5410);
+        if ((uint64_t)slot[y] >= (uint64_t)a.n_slots) continue;
+        const int place = (int)((uint32_t)slot[y] % kKv4Page);
+        uint8_t *half = half_record<D>(a, p, slot[y]);
+        const int at = p.is_v ? v_byte<D>(2 * (p.c & ~4) + (p.c >> 2 & 1), place) : k_byte<D>(2 * p.c);
+        *reinterpret_cast<uint32_t *>(half + place * R::kRow + at) = word;
         if ((p.c & 3) == 0)
             *reinterpret_cast<__nv_bfloat16 *>(half + R::kScales + place * R::kScaleRow + 2 * (p.c >> 2)) = s;
     }
 }
 
+// kHalves: halfwords of a thread, 16 bytes of output.
 template <int D, bool kF32, int kTokens>
 __global__ void __launch_bounds__(kKv4Threads) kv4_read_kernel(const Kv4CacheArgs a)
 {
     using R = Kv4Record<D>;
+    constexpr int kHalves = kF32 ? 1 : 2;
     pdl_launch_next();
-    const Kv4Place p = place_of<D / 4, kTokens>(a);
+    const Kv4Place p = place_of<D / (4 * kHalves), kTokens>(a);
+    const int h = p.c * kHalves;
     pdl_wait();
     int64_t slot[kTokens];
     uint32_t word[kTokens];
@@ -143,31 +148,31 @@ __global__ void __launch_bounds__(kKv4Threads) kv4_read_kernel(const Kv4CacheArg
     for (int y = 0; y < kTokens; ++y) slot[y] = p.token + y < a.tokens ? a.slots[p.token + y] : -1;
 #pragma unroll
     for (int y = 0; y < kTokens; ++y) {
-        word[y] = 0x8888u;
+        word[y] = 0x88888888u;
         s[y] = 0.f;
-        if (slot[y] >= 0 && slot[y] < a.n_slots) {
-            const int place = (int)(slot[y] % kKv4Page);
+        if ((uint64_t)slot[y] < (uint64_t)a.n_slots) {
+            const int place = (int)((uint32_t)slot[y] % kKv4Page);
             const uint8_t *half = half_record<D>(a, p, slot[y]), *row = half + place * R::kRow;
-            word[y] = *reinterpret_cast<const uint16_t *>(row + (p.is_v ? v_byte<D>(p.c, place) : k_byte<D>(p.c)));
-            s[y] = __bfloat162float(*reinterpret_cast<const __nv_bfloat16 *>(half + R::kScales + place * R::kScaleRow + 2 * (p.c >> 3)));
+            const uint8_t *first = row + (p.is_v ? v_byte<D>(h, place) : k_byte<D>(h));
+            word[y] = *reinterpret_cast<const uint16_t *>(first);
+            if (kHalves == 2) word[y] |= (uint32_t)*reinterpret_cast<const uint16_t *>(p.is_v ? row + v_byte<D>(h + 1, place) : first + 2) << 16;
+            s[y] = __bfloat162float(*reinterpret_cast<const __nv_bfloat16 *>(half + R::kScales + place * R::kScaleRow + 2 * (h >> 3)));
         }
     }
     void *out = p.is_v ? a.v_out : a.k_out;
 #pragma unroll
     for (int y = 0; y < kTokens; ++y) {
         if (p.token + y >= a.tokens) break;
-        float x[4];
+        float x[4 * kHalves];
 #pragma unroll
-        for (int i = 0; i < 4; ++i)  // (2^23 + u as a pattern)
+        for (int i = 0; i < 4 * kHalves; ++i)  // (2^23 + u as a pattern)
             x[i] = s[y] * (__uint_as_float((word[y] >> (4 * i) & 15u) | 0x4b000000u) - 8388616.f);
-        const int64_t at = ((p.token + y) * a.Hkv + p.head) * D + 4 * p.c;
-        if (kF32) {
+        const int64_t at = ((p.token + y) * a.Hkv + p.head) * D + 4 * h;
+        if constexpr (kF32)
             *reinterpret_cast<float4 *>(static_cast<float *>(out) + at) = make_float4(x[0], x[1], x[2], x[3]);
-        } else {
-            const __nv_bfloat162 lo = __floats2bfloat162_rn(x[0], x[1]), hi = __floats2bfloat162_rn(x[2], x[3]);
-            *reinterpret_cast<uint2 *>(static_cast<__nv_bfloat16 *>(out) + at) =
-                make_uint2(*reinterpret_cast<const uint32_t *>(&lo), *reinterpret_cast<const uint32_t *>(&hi));
-        }
+        else
+            *reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(out) + at) =
+                make_uint4(ptx::cvt_bf16x2(x[0], x[1]), ptx::cvt_bf16x2(x[2], x[3]), ptx::cvt_bf16x2(x[4], x[5]), ptx::cvt_bf16x2(x[6], x[7]));
     }
 }
 
@@ -259,7 +264,7 @@ extern "C" pa_status pa_kv4_read(const pa_kv4_pool *pool, int64_t n_tokens, cons
     int64_t ctas;
     bool many;
     if (dtype != PA_BF16 && dtype != PA_F32) return fail(PA_ERR_INVALID_ARG, "bad dtype");
-    if (pa_status s = cache_args(pool, pool ? pool->head_dim / 4 : 0, &many, n_tokens, kv_pool, slot_map, k_out, v_out, &a, &ctas)) return s;
+    if (pa_status s = cache_args(pool, pool ? pool->head_dim / (dtype == PA_F32 ? 4 : 8) : 0, &many, n_tokens, kv_pool, slot_map, k_out, v_out, &a, &ctas)) return s;
     if (ctas == 0) return PA_OK;
     a.pool = static_cast<uint8_t *>(const_cast<void *>(kv_pool));
     a.k_out = k_out;
