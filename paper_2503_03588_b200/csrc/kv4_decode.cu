@@ -180,7 +180,7 @@ struct Kv4Query {
         top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
         // f is q 2^10 / 2^e with 2^e <= max |q| < 2^(e + 1) (q 2^14 / 2^e where the nibbles come as u 2^-24): products are u q 2^(-10 - e).
         const uint32_t field = min(max(top >> 7, 27u), 243u);  // e + 127 (heads below 2^-100 lose bits; up to 2^116 they fit)
-        const float down = __uint_as_float((264u - field) << 23), up = __uint_as_float((field + 10u) << 23) * scale_log2;
+        const float down = __uint_as_float((264u - field) << 23), up = fmaxf(__uint_as_float((field + 10u) << 23) * scale_log2, 0x1p-126f);  // (above 0: times -inf it stays that)
         c0 = __shfl_sync(0xffffffffu, up, 8 * t);
         c1 = __shfl_sync(0xffffffffu, up, 8 * t + 4);
 #pragma unroll
@@ -890,6 +890,7 @@ __global__ void __launch_bounds__(kR4Threads, 1) kv4_range_kernel(const Kv4Args 
     }
     __syncthreads();
     if (*abort_flag) {
+        if (tid < 2 && !a.whole_rows) reinterpret_cast<int32_t *>(a.parts + ((int64_t)blockIdx.x * 2 + tid) * Kv4Part<D>::kFloats)[0] = -1;
         if (tid == 0) {  // copies that may still be in flight have a bounded time to land
             const long long t0 = clock64();
             while (clock64() - t0 < 2000000ll) {

@@ -349,6 +349,55 @@ def test_decode_kv4_a_wait_that_runs_out_ends_the_kernel(pa, pa_env, path, clust
         assert torch.equal(o, ref) and torch.equal(lse, ref_lse)
 
 
+def test_decode_kv4_a_wait_that_runs_out_leaves_nothing_to_merge(pa, pa_env):
+    """Under a limit of one cycle, on a workspace that never held a result: the kernel that merges rows takes nothing from it."""
+    pa_env(PA_DECODE_PATH="persist")
+    c = _Cache(pa, [5000 + 300 * i for i in range(30)], 4, 128, seed=14)
+    q = _randn(30, 28, 128).cuda()
+    ref, ref_lse, ws = pa.pa_decode_kv4(q, c.pool, c.table, c.lens_d, 60, 1)
+    guard = torch.full((3, *q.shape), 7.0, dtype=torch.bfloat16).cuda()
+    for byte in (0, 1, 127, 255):
+        ws.fill_(byte)
+        try:
+            pa.pa_set_wait_limit_cycles(1)
+            pa.pa_decode_kv4(q, c.pool, c.table, c.lens_d, 60, 1, o=guard[1], workspace=ws)
+            pa.pa_decode_status(ws)
+        except pa.PaError as err:
+            assert "PA_ERR_TIMEOUT" in str(err)
+        finally:
+            pa.pa_set_wait_limit_cycles(0)
+        assert (guard[0] == 7).all() and (guard[2] == 7).all()
+    o, lse, _ = pa.pa_decode_kv4(q, c.pool, c.table, c.lens_d, 60, 1, workspace=ws)
+    pa.pa_decode_status(ws)
+    assert torch.equal(o, ref) and torch.equal(lse, ref_lse)
+
+
+def test_decode_kv4_heads_of_zeros_under_a_tiny_scale(pa):
+    """The powers of two of a head of zeros times a small scale fall below fp32's range: still the mean of the values."""
+    c = _Cache(pa, [70, 1, 200], 2, 64, seed=15)
+    q = torch.zeros((3, 4, 64), dtype=torch.bfloat16).cuda()
+    ref = pa.pa_decode_kv4(q, c.pool, c.table, c.lens_d, 5, 1)
+    out = pa.pa_decode_kv4(q, c.pool, c.table, c.lens_d, 5, 1, softmax_scale=1e-30)
+    assert torch.equal(ref[0], out[0]) and torch.equal(ref[1], out[1]) and torch.isfinite(out[1]).all()
+
+
+def test_decode_kv4_on_two_streams_at_once(pa):
+    """Appends and decodes of two caches on two streams, every call with a workspace of its own."""
+    caches = [_Cache(pa, [3000 + 100 * i + 7 * s for i in range(40)], 4, 128, seed=16 + s) for s in range(2)]
+    q = _randn(40, 28, 128).cuda()
+    ref = [pa.pa_decode_kv4(q, c.pool, c.table, c.lens_d, 5, 1)[:2] for c in caches]
+    streams, got = [torch.cuda.Stream() for _ in range(2)], []
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                got.append((i, pa.pa_decode_kv4(q, caches[i].pool, caches[i].table, caches[i].lens_d, 5, 1)))
+    torch.cuda.synchronize()
+    for i, (o, lse, ws) in got:
+        assert torch.equal(o, ref[i][0]) and torch.equal(lse, ref[i][1])
+        pa.pa_decode_status(ws)
+
+
 # ------------------------------------------------------------------ together
 @pytest.mark.parametrize("captured", [False, True])
 def test_a_serving_run(pa, oracle, captured):
