@@ -431,12 +431,15 @@ PyObject *build_block_tables(PyObject *const *x)
     return tuple(cu, slots, positions, lens, left, ws);
 }
 
+// A stride, 0 for an axis of one entry (PyTorch leaves any number there).
+int64_t stride_of(const at::Tensor &t, int64_t axis) { return t.size(axis) > 1 ? t.stride(axis) : 0; }
+
 // Queries or keys [tokens, head, head_dim] or [batch, seq, head, head_dim].
 pa_strides token_strides(const at::Tensor &t)
 {
     expect((t.dim() == 3 || t.dim() == 4) && t.stride(-1) == 1,
            "expected [tokens, head, head_dim] or [batch, seq, head, head_dim] with contiguous head_dim");
-    return {t.dim() == 4 ? t.stride(0) : 0, t.stride(-3), t.stride(-2)};
+    return {t.dim() == 4 ? stride_of(t, 0) : 0, stride_of(t, -3), stride_of(t, -2)};
 }
 pa_rope_params rope_params(const at::Tensor &q, const at::Tensor &k, const at::Tensor &wq, const at::Tensor &wk,
                            const at::Tensor &cos_sin, const at::Tensor &positions, const at::Tensor &q_like, const at::Tensor &k_like,
@@ -520,7 +523,7 @@ pa_kv4_pool kv4_pool(const at::Tensor &pool, int64_t head_dim)
                pool.size(2) == (int64_t)pa_kv4_page_bytes((int32_t)head_dim),
            "expected a uint8 pool [n_pages, n_kv_heads, pa_kv4_page_bytes(head_dim)] with contiguous records");
     expect(pool.size(0) <= INT32_MAX && pool.size(1) <= INT32_MAX, "too large a size");
-    return {(int32_t)pool.size(1), (int32_t)head_dim, 64, (int32_t)pool.size(0), pool.stride(0), pool.stride(1)};
+    return {(int32_t)pool.size(1), (int32_t)head_dim, 64, (int32_t)pool.size(0), stride_of(pool, 0), stride_of(pool, 1)};
 }
 
 // k_new, v_new, kv_pool, slot_map
@@ -534,7 +537,7 @@ PyObject *kv4_append(PyObject *const *x)
     expect(p.n_kv_heads == k.size(1), "the pool has as many heads as k_new and v_new");
     on_current_device(k, v, pool, slots);
     run([&] {
-        return pa_kv4_append(&p, k.size(0), k.data_ptr(), v.data_ptr(), {0, k.stride(0), k.stride(1)}, {0, v.stride(0), v.stride(1)},
+        return pa_kv4_append(&p, k.size(0), k.data_ptr(), v.data_ptr(), {0, stride_of(k, 0), stride_of(k, 1)}, {0, stride_of(v, 0), stride_of(v, 1)},
                              pool.data_ptr(), (const int64_t *)slots.data_ptr(), stream());
     });
     Py_RETURN_NONE;

@@ -110,6 +110,8 @@ def test_kv4_refusals(b):
         for bad in (dict(head_dim=96), dict(block=32), dict(n_kv_heads=70000), dict(head_stride=9200), dict(page_stride=0)):
             assert call(_changed(good, **bad)) == "PA_ERR_SHAPE", bad
         assert call(_changed(good, head_stride=9224)) == "PA_ERR_ALIGNMENT"
+        for bad in (dict(page_stride=9216), dict(page_stride=4 * 9216 - 16), dict(head_stride=10 * 9216 - 16, page_stride=9216)):   # records over one another
+            assert call(_changed(good, **bad)) == "PA_ERR_SHAPE", bad
         assert call(None) == call(_changed(good), n=-1) == "PA_ERR_INVALID_ARG"
         assert call(_changed(good), n=0) == "PA_OK"                      # nothing to do, nothing launched
         assert call(_changed(good), n=1 << 50) == "PA_ERR_SHAPE"
