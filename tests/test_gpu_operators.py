@@ -263,3 +263,63 @@ def test_norm_rope_captured_and_replayed(pa):
     ref_out, ref = pa.pa_qk_norm_rope(*args), pa.pa_qk_norm_rope_backward(*args, *back)
     for a, b in zip((*out, *grads[:4]), (*ref_out, *ref[:4])):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("hq,hkv,d,rot", [(28, 4, 128, 128), (16, 4, 64, 32), (5, 3, 64, 48), (9, 2, 128, 16), (3, 1, 128, 0)])
+def test_norm_rope_many_tokens(pa, hq, hkv, d, rot, interleaved):
+    """Enough tokens for warps that stride over them, in two uneven shares: a batch of views into a projection's output, the
+    queries in place; tokens without a position among them keep what they hold, NaN and infinities too."""
+    n = 148 * 112 * 256 // d // (hq + hkv) // 2 + 1201
+    g = torch.Generator().manual_seed(21)
+    qkv = torch.randn((2, n, hq + 2 * hkv, d), generator=g).bfloat16().cuda()
+    _, _, wq, wk, cs, _ = _inputs(1, hq, hkv, d, rot, 22)
+    pos = torch.randint(0, cs.shape[0], (2, n), generator=g, dtype=torch.int32).cuda()
+    bad = (torch.rand((2, n), generator=g) < 0.1).cuda()
+    bad[:, -3:] = True
+    pos[bad] = torch.tensor([-1, cs.shape[0], -2 ** 31, 2 ** 31 - 1], dtype=torch.int32).cuda().repeat(n)[:int(bad.sum())]
+    qkv[bad] = float("nan")
+    qkv[0, -3:] = float("inf")
+    before = qkv.clone()
+    q, k = qkv[:, :, :hq], qkv[:, :, hq:hq + hkv]
+    ko = torch.full((2, n, hkv, d), 7.0, dtype=torch.bfloat16).cuda()
+    pa.pa_qk_norm_rope(q, k, wq, wk, cs, pos, q_out=q, k_out=ko, eps=1e-5, interleaved=interleaved)
+    good = ~bad
+    for i, (x, out) in enumerate(((before[:, :, :hq], q), (before[:, :, hq:hq + hkv], ko))):
+        _near_bf16(out[good], *plain.norm_rope(x[good], (wq, wk)[i], cs, pos[good], 1e-5, interleaved))
+    assert (ko[bad] == 7).all()
+    assert torch.equal(q[bad].view(torch.int16), before[:, :, :hq][bad].view(torch.int16))
+    assert torch.equal(qkv[:, :, hq:].view(torch.int16), before[:, :, hq:].view(torch.int16))
+
+
+def test_axes_of_one_entry_have_any_stride(pa):
+    """One token, one head, one batch entry: the strides of their axes are never used."""
+    g = torch.Generator().manual_seed(23)
+    x = torch.randn(4096, generator=g).bfloat16().cuda()
+    wq, wk, cs, pos = _inputs(1, 1, 1, 64, 64, 24)[2:]
+    odd = x.as_strided((1, 1, 1, 64), (3, 5, 7, 1))
+    out = pa.pa_qk_norm_rope(odd, odd, wq, wk, cs, pos)
+    ref = pa.pa_qk_norm_rope(odd.contiguous().view(1, 1, 64), odd.contiguous().view(1, 1, 64), wq, wk, cs, pos)
+    assert torch.equal(out[0].flatten(), ref[0].flatten()) and torch.equal(out[1].flatten(), ref[1].flatten())
+
+
+def test_calls_on_two_streams_at_once(pa):
+    """Tables, norms and gradients on two streams, each call with a workspace of its own, many times."""
+    args = [_inputs(3000, 8, 2, 128, 128, 30 + i) for i in range(2)]
+    back = [torch.randn((3000, h, 128)).cuda() for h in (8, 2)]
+    new, cached = _ints([40] * 500), _ints([100] * 500)
+    free, count = _ints(np.arange(1000)), _ints([900])
+    tables = lambda i: pa.pa_build_block_tables(new, cached, free[i:], count, torch.full((500, 4), -1, dtype=torch.int32).cuda(), 1000, 20000)  # noqa: E731
+    call = lambda i: (*pa.pa_qk_norm_rope(*args[i]), *pa.pa_qk_norm_rope_backward(*args[i], *back)[:4], *tables(i)[:5])  # noqa: E731
+    ref = [[x.clone() for x in call(i)] for i in range(2)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    got = []
+    for _ in range(20):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                got.append((i, call(i)))
+    torch.cuda.synchronize()
+    for i, outs in got:
+        for a, b in zip(outs, ref[i]):
+            assert torch.equal(a, b)
