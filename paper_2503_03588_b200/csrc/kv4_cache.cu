@@ -55,20 +55,6 @@ __device__ __forceinline__ uint8_t *half_record(const Kv4CacheArgs &a, const Kv4
     return a.pool + (int64_t)(uint32_t)((uint64_t)slot / kKv4Page) * a.page_stride + p.head * a.head_stride +
            (p.is_v ? Kv4Record<D>::kHalf : 0);
 }
-// Byte in its row at which the nibbles of features 4 h .. 4 h + 3 stand, a halfword.  (K: of features 8 c .. 8 c + 7, a word at the
-// place of h = 2 c.)
-template <int D>
-__device__ __forceinline__ int k_byte(int h)
-{
-    const int c = h >> 1;
-    return ((c & 3) * Kv4Record<D>::kGroups + (c >> 2)) * 4 + 2 * (h & 1);
-}
-template <int D>
-__device__ __forceinline__ int v_byte(int h, int place)
-{
-    return ((h & 7) ^ ((place & 2) << 1)) * (2 * Kv4Record<D>::kGroups) + 2 * (h >> 3);
-}
-
 __device__ __forceinline__ uint32_t max_magnitude(uint32_t a, uint32_t b)  // of two pairs of bf16 without sign; NaN stays
 {
     uint32_t d;
@@ -76,30 +62,36 @@ __device__ __forceinline__ uint32_t max_magnitude(uint32_t a, uint32_t b)  // of
     return d;
 }
 
+// A thread's features: half a group, j its number.  In K two words of their row, in V two halfwords each of the chunks of this group
+// and of its neighbour, which a thread of the neighbour's has the other halfwords of.
 template <int D, int kTokens>
 __global__ void __launch_bounds__(kKv4Threads) kv4_append_kernel(const Kv4CacheArgs a)
 {
     using R = Kv4Record<D>;
+    constexpr int NG = R::kGroups;
     pdl_launch_next();
-    const Kv4Place p = place_of<D / 8, kTokens>(a);  // (the threads of a group share its tokens)
+    const Kv4Place p = place_of<D / 16, kTokens>(a);  // (the threads of a head share its tokens)
+    const int j = p.c >> 1, half = p.c & 1;
     const int64_t st = p.is_v ? a.v_st : a.k_st;
-    const __nv_bfloat16 *src = p.is_v ? a.v + p.token * a.v_st + p.head * a.v_sh : a.k + p.token * a.k_st + p.head * a.k_sh;
+    const __nv_bfloat16 *src = (p.is_v ? a.v + p.head * a.v_sh : a.k + p.head * a.k_sh) + p.token * st + 16 * p.c;
     pdl_wait();
     int64_t slot[kTokens];
-    uint4 raw[kTokens];
+    uint4 raw[kTokens][2];
 #pragma unroll
     for (int y = 0; y < kTokens; ++y) {
         const bool in = p.token + y < a.tokens;
         slot[y] = in ? a.slots[p.token + y] : -1;
-        raw[y] = in ? *reinterpret_cast<const uint4 *>(src + y * st + 8 * p.c) : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+        for (int x = 0; x < 2; ++x) raw[y][x] = in ? *reinterpret_cast<const uint4 *>(src + y * st + 8 * x) : make_uint4(0u, 0u, 0u, 0u);
     }
 #pragma unroll
     for (int y = 0; y < kTokens; ++y) {
-        const uint32_t w[4] = {raw[y].x, raw[y].y, raw[y].z, raw[y].w};
+        const uint32_t w[8] = {raw[y][0].x, raw[y][0].y, raw[y][0].z, raw[y][0].w, raw[y][1].x, raw[y][1].y, raw[y][1].z, raw[y][1].w};
         constexpr uint32_t kAbs = 0x7fff7fffu;
-        uint32_t two = max_magnitude(max_magnitude(w[0] & kAbs, w[1] & kAbs), max_magnitude(w[2] & kAbs, w[3] & kAbs));
+        uint32_t two = w[0] & kAbs;
+#pragma unroll
+        for (int i = 1; i < 8; ++i) two = max_magnitude(two, w[i] & kAbs);
         two = max_magnitude(two, __shfl_xor_sync(0xffffffffu, two, 1));
-        two = max_magnitude(two, __shfl_xor_sync(0xffffffffu, two, 2));
         const uint32_t top = max(two & 0xffffu, two >> 16);  // (patterns without sign are ordered as integers, NaN on top)
         // s = amax / 7 in bf16.  A quotient by 7 is never near enough to the middle of two bf16 numbers for the fp32 product to
         // round differently (it is 1/14 of a step away at least).
@@ -112,70 +104,91 @@ __global__ void __launch_bounds__(kKv4Threads) kv4_append_kernel(const Kv4CacheA
         const float inv = zero || wild ? 0.f : __fdividef(1.0f - 0x1p-16f, __bfloat162float(s));
         constexpr float kMagic = 12582912.f + 8.f;
         constexpr uint32_t kPattern = 0x4b400000u, kAll = 0x11111111u;
-        uint32_t word = 0;
+        const uint64_t inv2 = ptx::pack_f32x2(inv, inv), magic2 = ptx::pack_f32x2(kMagic, kMagic);
+        uint32_t word[2];
 #pragma unroll
-        for (int i = 3; i >= 0; --i) {
-            const uint32_t n0 = __float_as_uint(fmaf(__uint_as_float(w[i] << 16), inv, kMagic));
-            const uint32_t n1 = __float_as_uint(fmaf(__uint_as_float(w[i] & 0xffff0000u), inv, kMagic));
-            word = (word * 16u + n1) * 16u + n0;
+        for (int x = 0; x < 2; ++x) {
+            word[x] = 0;
+#pragma unroll
+            for (int i = 3; i >= 0; --i) {
+                const uint32_t z = w[4 * x + i];
+                float n0, n1;
+                ptx::unpack_f32x2(ptx::fma_f32x2(ptx::pack_f32x2(__uint_as_float(z << 16), __uint_as_float(z & 0xffff0000u)), inv2, magic2), n0, n1);
+                word[x] = (word[x] * 16u + __float_as_uint(n1)) * 16u + __float_as_uint(n0);
+            }
+            word[x] -= kPattern * kAll;
         }
-        word -= kPattern * kAll;
-        // V: its two halfwords belong into two chunks.  The thread with the same features of the next group has their neighbours,
-        // and each of the two takes a chunk.
-        const uint32_t other = __shfl_xor_sync(0xffffffffu, word, 4);
-        if (p.is_v) word = __byte_perm(word, other, p.c & 4 ? 0x3276 : 0x5410);
+        // V: of the chunks 4 half + {0, 1}, {2, 3} the even groups' threads take the even ones, for two groups each.
+        const uint32_t got = __shfl_xor_sync(0xffffffffu, __byte_perm(word[0], word[1], j & 1 ? 0x5410 : 0x7632), 2);
+        if (p.is_v) {
+            word[0] = __byte_perm(word[0], got, j & 1 ? 0x3254 : 0x5410);
+            word[1] = __byte_perm(word[1], got, j & 1 ? 0x3276 : 0x7610);
+        }
         if ((uint64_t)slot[y] >= (uint64_t)a.n_slots) continue;
         const int place = (int)((uint32_t)slot[y] % kKv4Page);
-        uint8_t *half = half_record<D>(a, p, slot[y]);
-        const int at = p.is_v ? v_byte<D>(2 * (p.c & ~4) + (p.c >> 2 & 1), place) : k_byte<D>(2 * p.c);
-        *reinterpret_cast<uint32_t *>(half + place * R::kRow + at) = word;
-        if ((p.c & 3) == 0)
-            *reinterpret_cast<__nv_bfloat16 *>(half + R::kScales + place * R::kScaleRow + 2 * (p.c >> 2)) = s;
+        uint8_t *record = half_record<D>(a, p, slot[y]);
+        const int at = p.is_v ? (4 * (half ^ (place >> 1 & 1)) + (j & 1)) * (2 * NG) + 2 * (j & ~1) : 8 * NG * half + 4 * j;
+        uint32_t *to = reinterpret_cast<uint32_t *>(record + place * R::kRow + at);
+        to[0] = word[0];
+        to[NG] = word[1];
+        if (half == 0) *reinterpret_cast<__nv_bfloat16 *>(record + R::kScales + place * R::kScaleRow + 2 * j) = s;
     }
 }
 
-// kHalves: halfwords of a thread, 16 bytes of output.
+// A thread's features: 4 g + (0 .. 3) of two groups, 2 jj and 2 jj + 1, whose scales are a word, whose nibbles in V are one and in K halves
+// of two.  Its stores are its neighbours' neighbours.
 template <int D, bool kF32, int kTokens>
 __global__ void __launch_bounds__(kKv4Threads) kv4_read_kernel(const Kv4CacheArgs a)
 {
     using R = Kv4Record<D>;
-    constexpr int kHalves = kF32 ? 1 : 2;
+    constexpr int NG = R::kGroups;
     pdl_launch_next();
-    const Kv4Place p = place_of<D / (4 * kHalves), kTokens>(a);
-    const int h = p.c * kHalves;
+    const Kv4Place p = place_of<D / 8, kTokens>(a);
+    const int g = p.c & 7, jj = p.c >> 3;
     pdl_wait();
     int64_t slot[kTokens];
-    uint32_t word[kTokens];
-    float s[kTokens];
+    uint32_t word[kTokens], scale[kTokens];
 #pragma unroll
     for (int y = 0; y < kTokens; ++y) slot[y] = p.token + y < a.tokens ? a.slots[p.token + y] : -1;
 #pragma unroll
     for (int y = 0; y < kTokens; ++y) {
         word[y] = 0x88888888u;
-        s[y] = 0.f;
+        scale[y] = 0u;
         if ((uint64_t)slot[y] < (uint64_t)a.n_slots) {
             const int place = (int)((uint32_t)slot[y] % kKv4Page);
-            const uint8_t *half = half_record<D>(a, p, slot[y]), *row = half + place * R::kRow;
-            const uint8_t *first = row + (p.is_v ? v_byte<D>(h, place) : k_byte<D>(h));
-            word[y] = *reinterpret_cast<const uint16_t *>(first);
-            if (kHalves == 2) word[y] |= (uint32_t)*reinterpret_cast<const uint16_t *>(p.is_v ? row + v_byte<D>(h + 1, place) : first + 2) << 16;
-            s[y] = __bfloat162float(*reinterpret_cast<const __nv_bfloat16 *>(half + R::kScales + place * R::kScaleRow + 2 * (h >> 3)));
+            const uint8_t *record = half_record<D>(a, p, slot[y]), *row = record + place * R::kRow;
+            scale[y] = *reinterpret_cast<const uint32_t *>(record + R::kScales + place * R::kScaleRow + 4 * jj);
+            if (p.is_v) {
+                word[y] = *reinterpret_cast<const uint32_t *>(row + (g ^ ((place & 2) << 1)) * (2 * NG) + 4 * jj);
+            } else {
+                const uint2 both = *reinterpret_cast<const uint2 *>(row + (g >> 1) * (4 * NG) + 8 * jj);
+                word[y] = __byte_perm(both.x, both.y, g & 1 ? 0x7632 : 0x5410);
+            }
         }
     }
+    const int64_t to = (p.token * a.Hkv + p.head) * D + 64 * jj + 4 * g, step = (int64_t)a.Hkv * D;
     void *out = p.is_v ? a.v_out : a.k_out;
 #pragma unroll
     for (int y = 0; y < kTokens; ++y) {
         if (p.token + y >= a.tokens) break;
-        float x[4 * kHalves];
 #pragma unroll
-        for (int i = 0; i < 4 * kHalves; ++i)  // (2^23 + u as a pattern)
-            x[i] = s[y] * (__uint_as_float((word[y] >> (4 * i) & 15u) | 0x4b000000u) - 8388616.f);
-        const int64_t at = ((p.token + y) * a.Hkv + p.head) * D + 4 * h;
-        if constexpr (kF32)
-            *reinterpret_cast<float4 *>(static_cast<float *>(out) + at) = make_float4(x[0], x[1], x[2], x[3]);
-        else
-            *reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(out) + at) =
-                make_uint4(ptx::cvt_bf16x2(x[0], x[1]), ptx::cvt_bf16x2(x[2], x[3]), ptx::cvt_bf16x2(x[4], x[5]), ptx::cvt_bf16x2(x[6], x[7]));
+        for (int x = 0; x < 2; ++x) {
+            const float s = __uint_as_float(x ? scale[y] & 0xffff0000u : scale[y] << 16);
+            const uint64_t s2 = ptx::pack_f32x2(s, s), off2 = ptx::pack_f32x2(-8388616.f, -8388616.f);
+            auto two = [&](int i) {  // (2^23 + u as a pattern)
+                const uint32_t u = word[y] >> (16 * x + 4 * i);
+                return ptx::mul_f32x2(s2, ptx::add_f32x2(ptx::pack_f32x2(__uint_as_float((u & 15u) | 0x4b000000u),
+                                                                         __uint_as_float((u >> 4 & 15u) | 0x4b000000u)), off2));
+            };
+            float v0, v1, v2, v3;
+            ptx::unpack_f32x2(two(0), v0, v1);
+            ptx::unpack_f32x2(two(2), v2, v3);
+            const int64_t at = to + y * step + 32 * x;
+            if constexpr (kF32)
+                *reinterpret_cast<float4 *>(static_cast<float *>(out) + at) = make_float4(v0, v1, v2, v3);
+            else
+                *reinterpret_cast<uint2 *>(static_cast<__nv_bfloat16 *>(out) + at) = make_uint2(ptx::cvt_bf16x2(v0, v1), ptx::cvt_bf16x2(v2, v3));
+        }
     }
 }
 
@@ -240,7 +253,7 @@ extern "C" pa_status pa_kv4_append(const pa_kv4_pool *pool, int64_t n_tokens, co
     Kv4CacheArgs a;
     int64_t ctas;
     bool many;
-    if (pa_status s = cache_args(pool, pool ? pool->head_dim / 8 : 0, &many, n_tokens, kv_pool, slot_map, k_new, v_new, &a, &ctas)) return s;
+    if (pa_status s = cache_args(pool, pool ? pool->head_dim / 16 : 0, &many, n_tokens, kv_pool, slot_map, k_new, v_new, &a, &ctas)) return s;
     for (const pa_strides &s : {k_strides, v_strides}) {
         if (s.seq < 0 || s.head < 0) return fail(PA_ERR_SHAPE, "strides must be >= 0");
         if ((s.seq % 8) || (s.head % 8)) return fail(PA_ERR_ALIGNMENT, "strides must be multiples of 8 elements (16 bytes)");
@@ -270,7 +283,7 @@ extern "C" pa_status pa_kv4_read(const pa_kv4_pool *pool, int64_t n_tokens, cons
     int64_t ctas;
     bool many;
     if (dtype != PA_BF16 && dtype != PA_F32) return fail(PA_ERR_INVALID_ARG, "bad dtype");
-    if (pa_status s = cache_args(pool, pool ? pool->head_dim / (dtype == PA_F32 ? 4 : 8) : 0, &many, n_tokens, kv_pool, slot_map, k_out, v_out, &a, &ctas)) return s;
+    if (pa_status s = cache_args(pool, pool ? pool->head_dim / 8 : 0, &many, n_tokens, kv_pool, slot_map, k_out, v_out, &a, &ctas)) return s;
     if (ctas == 0) return PA_OK;
     a.pool = static_cast<uint8_t *>(const_cast<void *>(kv_pool));
     a.k_out = k_out;
