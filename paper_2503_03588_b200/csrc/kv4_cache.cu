@@ -1,14 +1,13 @@
 // pa_kv4_append, pa_kv4_read: tokens into and out of the 4-bit pages.
 //
-// Bound by memory and, where 64 warps an SM do not hide it, by a token's chain from slot to page: append reads 2 bytes a number and
-// writes 9/16, read the other way round.  A thread has the same features of the same head, of K or of V, of kTokens = 4 tokens, so
-// that what it has to work out about its place is shared and four loads are on their way at once; of one where all run at once
-// anyhow (256 tokens of 4 heads of 128 features, append and read: 3.2 us, with four tokens a thread 5.0).
-// Append: eight features (16 bytes in, one 32-bit word of nibbles out), the four threads of a group share its largest
-// magnitude by shuffles.  Read: one 16-byte store, four features of fp32 or eight of bf16.
-// Measured, 153600 tokens of 4 heads of 128 features: append 81 us, 4.95 TB/s; read as fp32 126 us, 5.70 TB/s, as bf16 86 us,
-// 4.68 TB/s.  (CTAs of 256 threads: 82, 134 and 90; two tokens a thread 89, 156 and 94; eight 83, 134 and 108; appending by CTAs
-// that stay and have the next tokens on their way: 91.)
+// Bound by memory: append reads 2 bytes a number and writes 9/16, read the other way round.  Instructions are next (the first form,
+// eight and four features a thread, had three times as many and took 86 and 134 us for what is measured below), so a thread takes
+// 16 or 8 features of a head, of K or of V, and of four tokens: what it has to work out about its place is shared, and the loads of
+// four tokens are on their way at once.  The two threads of a group share its largest magnitude by a shuffle.
+// Measured, 153600 tokens of 4 heads of 128 features: append 61 us, 6.6 TB/s; read as fp32 116 us, 6.2 TB/s, as bf16 89 us,
+// 4.5 TB/s (chains from slot to page).  A token a thread where all threads run at once anyhow: 256 tokens, append and read, 3.1 us
+// and with four tokens a thread 5.0; read alone, 4000 tokens 5.2 and 5.0, 8000 tokens 9.3 and 7.3.
+// CTAs of 256 threads: append 64 us; two tokens a thread: the same within 3 %.
 #include <limits.h>
 
 #include "common.cuh"
@@ -230,7 +229,7 @@ static pa_status cache_args(const pa_kv4_pool *p, int per, bool *many, int64_t n
     a->n_slots = (int64_t)p->n_pages * kKv4Page;
     a->Hkv = p->n_kv_heads;
     if (n_tokens > INT_MAX / p->n_kv_heads) return fail(PA_ERR_SHAPE, "too many tokens");
-    *many = n_tokens * 2 * p->n_kv_heads * per > 148 * 2048;
+    *many = n_tokens * 2 * p->n_kv_heads * per > 148 * 2048;  // (measured on both sides: see above)
     const int tokens = *many ? 4 : 1;
     const int64_t rows = (n_tokens + tokens - 1) / tokens * 2 * p->n_kv_heads;
     *ctas = (rows * per + kKv4Threads - 1) / kKv4Threads;
