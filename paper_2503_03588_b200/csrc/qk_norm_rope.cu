@@ -1,10 +1,15 @@
 // pa_qk_norm_rope and its backward pass: root-mean-square norm of every query and key head and rotation by the
 // token's position, in one pass over both tensors.
 //
-// Bound by memory: a head is read and written once (backward: the head, its output's gradient, its gradient).  D / 8 lanes
-// share a head, eight features each: four pairs that belong together under the rotation, so that nothing but the norm's sums
-// crosses lanes.  A warp works on 256 / D heads of one token at a time, two numbers an instruction, and keeps what the token's heads share
-// in registers.
+// With r = 1 / sqrt(mean x^2 + eps), x^ = x r: out = R(pos) (x^ w).  Back: g = R(pos)^T d_out, dw = sum g x^, h = g w,
+// dx = r (h - x^ mean(h x^)).  Sums, means and products in fp32, one rounding at the end.
+//
+// Bound by memory: a head is read and written once (backward: the head, its output's gradient, its gradient).  D / 8 or D / 16 lanes
+// share a head, each with pairs that belong together under the rotation, so that nothing but the norm's sums crosses lanes;
+// arithmetic goes two numbers an instruction, and what a token's heads share stays in registers.
+// Measured, 28 and 4 heads of 128 features, 32768 tokens: forward 90 us (554 MB, 0.94 of a copy's rate), backward with fp32
+// gradients 172 us (1074 MB, 0.95); 8 tokens forward 2.0 us; 4505 tokens of 16 and 4 heads of 64 features forward 8.2 us, backward
+// 10.9 us (two kernels).
 #include <cuda_bf16.h>
 #include <math.h>
 
@@ -246,6 +251,7 @@ __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_grou
 // Forward.  Warps stride over the tokens, 512 / D heads at a time, queries, then keys.  A lane has sixteen features here, two times
 // eight numbers as above: half the instructions a head.  What a lane will need of the next kRopeAhead turns is on its way to
 // places of its own in shared memory (nobody else reads them, so there is nothing to wait for but its own copies).
+// (32768 tokens of 28 and 4 heads of 128: 90 us; with the next heads in registers 104, with a warp per few heads 100.)
 constexpr int kRopeAhead = 8;
 constexpr int kRopeTurn = 32 * 32;  // bytes of a turn: 32 of a lane
 
@@ -351,8 +357,9 @@ __global__ void __launch_bounds__(kBackThreads, 2) rope_kernel(const RopeArgs a)
     copies_wait<0>();
 }
 
-// Backward.  Warps stride over the tokens and keep the weights' gradients in registers; at the end a CTA adds its warps' up, in
-// their order, and leaves the sums for rope_weights_kernel.
+// Backward.  Warps stride over the tokens and keep the weights' gradients in registers, and the next heads' numbers; at the end a CTA
+// adds its warps' up, in their order, and leaves the sums for rope_weights_kernel.  Two CTAs of 128 registers a thread an SM (172 us
+// for the call above; smaller CTAs that keep less on its way 200 to 250).
 template <int D, bool kPairs, typename T>
 __global__ void __launch_bounds__(kBackThreads, 2) rope_backward_kernel(const RopeArgs a)
 {
