@@ -13,6 +13,8 @@
 #include <cuda_bf16.h>
 #include <math.h>
 
+#include <type_traits>
+
 #include "common.cuh"
 #include "sm100_ptx.cuh"
 
@@ -360,17 +362,23 @@ __global__ void __launch_bounds__(kBackThreads, 2) rope_kernel(const RopeArgs a)
 // Backward.  Warps stride over the tokens and keep the weights' gradients in registers, and the next heads' numbers; at the end a CTA
 // adds its warps' up, in their order, and leaves the sums for rope_weights_kernel.  Two CTAs of 128 registers a thread an SM (172 us
 // for the call above; smaller CTAs that keep less on its way 200 to 250).
-template <int D, bool kPairs, typename T>
+// kSplit: a token's heads, kBatch x 256 / D at a time, are dealt to a.chunks warps.
+constexpr int kBatch = 2;
+template <int D, bool kPairs, typename T, bool kSplit>
 __global__ void __launch_bounds__(kBackThreads, 2) rope_backward_kernel(const RopeArgs a)
 {
-    constexpr int kLanes = D / 8, kHeads = 32 / kLanes, kBatch = 2;
+    constexpr int kLanes = D / 8, kHeads = 32 / kLanes;
     __shared__ float sums[kBackWarps * kHeads][2][D];
     pdl_launch_next();
     const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, l = lane % kLanes, mine = lane / kLanes;
     const Pieces p = pieces_of<D, kPairs, 4>(l, a.half);
     Eight dw[2] = {};
     pdl_wait();
-    for (int64_t token = (int64_t)blockIdx.x * kBackWarps + wid; token < a.tokens; token += (int64_t)gridDim.x * kBackWarps) {
+    const int parts = kSplit ? a.chunks : 1, stride = parts * kBatch * kHeads;
+    const int64_t items = kSplit ? a.tokens * parts : a.tokens;
+    for (int64_t item = (int64_t)blockIdx.x * kBackWarps + wid; item < items; item += (int64_t)gridDim.x * kBackWarps) {
+        const int64_t token = kSplit ? (int64_t)((uint32_t)item / (uint32_t)parts) : item;  // (few items: see the launch)
+        const int part = kSplit ? (int)(item - token * parts) : 0;
         const int32_t pos = a.positions[token];
         const bool there = pos >= 0 && pos < a.max_positions;
         const int64_t b = token / a.seq, n = token - b * a.seq;
@@ -380,9 +388,13 @@ __global__ void __launch_bounds__(kBackThreads, 2) rope_backward_kernel(const Ro
         for (int which = 0; which < 2; ++which) {
             const int H = which ? a.Hkv : a.Hq;
             const pa_strides &sx = which ? a.sk : a.sq, &sd = which ? a.sko : a.sqo;
-            const __nv_bfloat16 *x = (which ? a.k : a.q) + b * sx.batch + n * sx.seq + mine * sx.head;
-            const T *d = static_cast<const T *>(which ? a.d_k : a.d_q) + b * sd.batch + n * sd.seq + mine * sd.head;
-            __nv_bfloat16 *out = (which ? a.k_out : a.q_out) + (token * H + mine) * D;
+            // The first heads of this part: the keys' follow the queries' in turn.
+            int first = 0;
+            if (kSplit) first = kBatch * kHeads * (which ? (part + parts - (a.Hq + kBatch * kHeads - 1) / (kBatch * kHeads) % parts) % parts : part);
+            if (kSplit && first >= H) continue;
+            const __nv_bfloat16 *x = (which ? a.k : a.q) + b * sx.batch + n * sx.seq + (first + mine) * sx.head;
+            const T *d = static_cast<const T *>(which ? a.d_k : a.d_q) + b * sd.batch + n * sd.seq + (first + mine) * sd.head;
+            __nv_bfloat16 *out = (which ? a.k_out : a.q_out) + (token * H + first + mine) * D;
             uint2 ra[kBatch], rb[kBatch];
             uint4 da[kBatch], db[kBatch];
             auto load = [&](int h) {
@@ -405,16 +417,16 @@ __global__ void __launch_bounds__(kBackThreads, 2) rope_backward_kernel(const Ro
                         }
                     }
                 }
-                x += kBatch * kHeads * sx.head;
-                d += kBatch * kHeads * sd.head;
+                x += stride * sx.head;
+                d += stride * sd.head;
             };
-            load(0);
+            load(first);
             const Eight w = load_weights<kPairs>(which ? a.k_weight : a.q_weight, a.w_f32, p);
             if (!looked_up) {
                 t = load_angles<kPairs>(a, p, there ? pos : 0);
                 looked_up = true;
             }
-            for (int h = 0; h < H; h += kBatch * kHeads) {
+            for (int h = first; h < H; h += stride) {
                 Eight v[kBatch], g[kBatch];
 #pragma unroll
                 for (int y = 0; y < kBatch; ++y) {
@@ -426,7 +438,7 @@ __global__ void __launch_bounds__(kBackThreads, 2) rope_backward_kernel(const Ro
                     else
                         g[y] = from_bf16<kPairs>(make_uint2(da[y].x, da[y].y), make_uint2(db[y].x, db[y].y));
                 }
-                if (h + kBatch * kHeads < H) load(h + kBatch * kHeads);
+                if (h + stride < H) load(h + stride);
 #pragma unroll
                 for (int y = 0; y < kBatch; ++y) {
                     const bool in = h + y * kHeads + mine < H;
@@ -460,6 +472,7 @@ __global__ void __launch_bounds__(kBackThreads, 2) rope_backward_kernel(const Ro
                     if (in) write_bf16<kPairs>(dx, out + p.a, out + p.b);
                     out += kHeads * D;
                 }
+                if (kSplit) out += (stride - kBatch * kHeads) * D;
             }
         }
     }
@@ -575,14 +588,24 @@ static pa_status rope_args(const pa_rope_params *p, const void *q, const void *k
 
 // CTAs of the kernels that stride over the tokens, a warp a token: two per SM (the workspace holds a part for each).
 constexpr int64_t kRopeCtas = 148 * 2;
-static int64_t token_ctas(const pa_rope_params *p)
+static int64_t token_ctas(const pa_rope_params *p, int64_t per_token = 1)
 {
-    const int64_t need = ((int64_t)p->batch * p->seq_len + kBackWarps - 1) / kBackWarps;
+    const int64_t need = ((int64_t)p->batch * p->seq_len * per_token + kBackWarps - 1) / kBackWarps;
     return need < kRopeCtas ? need : kRopeCtas;
 }
+// Backward: the warps that a token's heads are dealt to, as many as leave every warp one item.  Measured (us, backward alone, dealt and
+// not): 28 and 4 heads of 128 features, 7 tokens 4.6 and 8.7, 300 tokens 6.7 and 9.2, 1100 tokens 9.8 and 12.4; 16 and 4 heads of 64,
+// 64 tokens 4.2 and 5.1, 1100 tokens 6.4 and 7.0.
+static int64_t backward_parts(const pa_rope_params *p)
+{
+    const int64_t tokens = (int64_t)p->batch * p->seq_len, at_once = kBatch * 256 / p->head_dim;
+    const int64_t most = (p->n_q_heads + at_once - 1) / at_once + (p->n_kv_heads + at_once - 1) / at_once;
+    const int64_t room = kRopeCtas * kBackWarps / tokens;
+    return room < 1 ? 1 : room < most ? room : most;
+}
 // Up to this many warps of one piece each, else the persistent ones that ring.  Measured (us, one piece a warp and persistent):
-// 28 and 4 heads of 128 features, 600 tokens 4.6 and 6.5, 1200 tokens 7.5 and 7.2, 2500 tokens 14.0 and 10.3; 16 and 4 heads of
-// 64, 1200 tokens 3.4 and 4.5, 2500 tokens 5.5 and 6.1, 5000 tokens 9.4 and 8.7.
+// 28 and 4 heads of 128 features, 600 tokens 4.6 and 6.5, 1200 tokens 7.5 and 7.3, 2500 tokens 14.1 and 10.6; 16 and 4 heads of
+// 64, 1200 tokens 3.4 and 4.5, 3500 tokens 6.8 and 7.5, 4736 tokens 8.7 and 7.6.
 constexpr int64_t kRopeFewWarps = 148 * 112;
 
 }  // namespace pa
@@ -630,7 +653,7 @@ extern "C" size_t pa_qk_norm_rope_backward_workspace_bytes(const pa_rope_params 
 {
     using namespace pa;
     if (check_rope(p) != PA_OK) return 0;
-    return (size_t)token_ctas(p) * 2 * p->head_dim * sizeof(float);
+    return (size_t)token_ctas(p, backward_parts(p)) * 2 * p->head_dim * sizeof(float);
 }
 
 extern "C" pa_status pa_qk_norm_rope_backward(const pa_rope_params *p, const void *q, const void *k, const void *q_weight,
@@ -656,15 +679,20 @@ extern "C" pa_status pa_qk_norm_rope_backward(const pa_rope_params *p, const voi
     a.d_q = d_q_out;
     a.d_k = d_k_out;
     a.parts = static_cast<float *>(workspace);
-    const int64_t ctas = token_ctas(p);
+    const int64_t parts = backward_parts(p), ctas = token_ctas(p, parts);
+    a.chunks = (int32_t)parts;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    using bf16 = __nv_bfloat16;
-    static void (*const kernels[2][2][2])(const RopeArgs) = {{{rope_backward_kernel<64, false, bf16>, rope_backward_kernel<64, false, float>},
-                                                              {rope_backward_kernel<64, true, bf16>, rope_backward_kernel<64, true, float>}},
-                                                             {{rope_backward_kernel<128, false, bf16>, rope_backward_kernel<128, false, float>},
-                                                              {rope_backward_kernel<128, true, bf16>, rope_backward_kernel<128, true, float>}}};
-    auto launch = [&](auto kernel) { return launch_pdl(kernel, dim3((unsigned)ctas), kBackThreads, 0, st, a); };
-    PA_CUDA_OK(launch(kernels[p->head_dim == 128][p->interleaved != 0][d_dtype == PA_F32]));
+    auto launch = [&](auto split) {
+        constexpr bool S = decltype(split)::value;
+        using bf16 = __nv_bfloat16;
+        static void (*const kernels[2][2][2])(const RopeArgs) = {
+            {{rope_backward_kernel<64, false, bf16, S>, rope_backward_kernel<64, false, float, S>},
+             {rope_backward_kernel<64, true, bf16, S>, rope_backward_kernel<64, true, float, S>}},
+            {{rope_backward_kernel<128, false, bf16, S>, rope_backward_kernel<128, false, float, S>},
+             {rope_backward_kernel<128, true, bf16, S>, rope_backward_kernel<128, true, float, S>}}};
+        return launch_pdl(kernels[p->head_dim == 128][p->interleaved != 0][d_dtype == PA_F32], dim3((unsigned)ctas), kBackThreads, 0, st, a);
+    };
+    PA_CUDA_OK(parts > 1 ? launch(std::true_type()) : launch(std::false_type()));
     PA_CUDA_OK(launch_pdl(rope_weights_kernel, dim3((unsigned)(2 * p->head_dim / 8)), kSumThreads, 0, st,
                           static_cast<const float *>(a.parts), (int)ctas, (int)p->head_dim, dq_weight, dk_weight));
     return PA_OK;

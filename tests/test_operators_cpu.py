@@ -90,7 +90,7 @@ def test_rope_refusals(b):
     assert backward(_changed(good), 10, P + 2) == "PA_ERR_ALIGNMENT"
     assert backward(_changed(good), ws=0) == backward(_changed(good), ws_bytes=100) == "PA_ERR_WORKSPACE"
     assert backward(_changed(good), ws=P + 4) == "PA_ERR_ALIGNMENT"
-    assert b.lib.pa_qk_norm_rope_backward_workspace_bytes(_changed(good)) == 13 * 2 * 128 * 4   # CTAs of eight tokens
+    assert b.lib.pa_qk_norm_rope_backward_workspace_bytes(_changed(good)) == 25 * 2 * 128 * 4   # CTAs of eight warps, two warps a token
 
 
 def test_kv4_refusals(b):
