@@ -21,6 +21,14 @@ struct Kv4Record {  // of a page and KV head, in bytes
     static constexpr int kBytes = 2 * kHalf;               // 72 D
 };
 
+// How long a CTA of a cluster outlives a wait of its own that ran out, at most (in cycles): until each of its R peers has pushed its
+// part of a row of `blocks` blocks, which takes a peer a wait of up to `limit` for each of its blocks and one more for the barrier of
+// the cluster.  (Two million cycles a wait for the work itself.)  The table's length has no part in it.
+__host__ __device__ inline long long kv4_outlast_cycles(long long limit, int32_t blocks, int32_t R)
+{
+    return (limit + 2000000ll) * (2 + (blocks + R - 1) / R);
+}
+
 // Checks of a pool's description, shared by the entry points.
 pa_status check_kv4_pool(const pa_kv4_pool &p);
 

@@ -596,7 +596,7 @@ __global__ void __launch_bounds__(kC4Threads, 2) kv4_cluster_kernel(const Kv4Arg
             if (!ptx::mbar_wait_bounded_cluster(bar_recv, 0, abort_flag, a.status, 3, a.wait_cycles, (int)PA_ERR_TIMEOUT)) {
                 // This CTA's shared memory has to last until every peer's part is in it: a peer is there after a wait for each
                 // of its blocks at most, so this is over before its own limit is.
-                const long long t0 = clock64(), most = 4 * (a.wait_cycles + 2000000ll) * (2 + (int64_t)a.table_stride / R);
+                const long long t0 = clock64(), most = kv4_outlast_cycles(a.wait_cycles, n, R);
                 while (!ptx::mbar_try_wait_cluster(bar_recv, 0) && clock64() - t0 < most) {
                 }
             } else {
