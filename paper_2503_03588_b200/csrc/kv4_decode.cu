@@ -14,8 +14,8 @@
 //
 // The nibbles become 16-bit numbers without conversions.  K: w & 0x000f000f is two fp16 subnormals, u 2^-24, and w & 0x00f000f0 is
 // 16 times as much, for which the queries of the former are multiplied by 16; -8 sum_i q_i is what the accumulator starts
-// with.  V: (w & 0x000f000f) | 0x4300 is 128 + u in bf16, and a second product with a constant matrix of -136 takes off what is too
-// much, a tile of keys at a time, so that nothing large is carried along (fp32 outputs: an addition).  K rows are stored so that
+// with.  V: (w & 0x000f000f) | 0x4300 is 128 + u in bf16, and an addition of -136 leaves u - 8.  (Products of 128 + u from which others are
+// taken off would be 20 times the values, and overflow where the values do not.)  K rows are stored so that
 // a thread's 16 bytes hold its share of every group; V rows so that the same halfwords of two tokens, put side by side by a byte
 // permutation, are the fragments' key pairs.  Shared memory is read without bank conflicts and without ldmatrix.
 //
@@ -39,7 +39,10 @@ constexpr int kD4MaxGroup = 8;
 constexpr size_t kD4StatusBytes = 256;
 constexpr int kD4MaxSmem = 226 * 1024;  // (227 KB less some static shared memory)
 constexpr long long kD4WaitCycles = 2000000000ll;  // ~1 s
-constexpr float kD4Grow = 6.f;  // the maximum moves once it is exceeded by more than this (weights up to 2^6)
+// Weights are 2^(S - m).  m is set this far above the largest logit so far and moves once a logit exceeds it: no weight is above 1
+// (values as large as fp32 holds are summed without overflow where the sum by the true weights has none), and sums are rescaled
+// seldom.
+constexpr float kD4Grow = 6.f;
 
 struct Kv4Args {
     const __nv_bfloat16 *q;
@@ -87,13 +90,11 @@ __device__ __forceinline__ uint32_t and_or(uint32_t a, uint32_t b, uint32_t c)
 // The lowest nibble of each half of a word as fp16 u 2^-24, and the one above it as u 2^-20.
 __device__ __forceinline__ uint32_t nib_lo(uint32_t w) { return w & 0x000f000fu; }
 __device__ __forceinline__ uint32_t nib_hi(uint32_t w) { return w & 0x00f000f0u; }
-// The lowest nibble of each half as bf16 128 + u, or u - 8.
-__device__ __forceinline__ uint32_t nib_over(uint32_t w) { return and_or(w, 0x000f000fu, 0x43004300u); }
-constexpr uint32_t kMinus136 = 0xc308c308u;
+// The lowest nibble of each half as bf16 u - 8: 128 + u, less 136.
 __device__ __forceinline__ uint32_t nib_bf16(uint32_t w)
 {
     uint32_t d;
-    asm("add.rn.bf16x2 %0, %1, %2;\n" : "=r"(d) : "r"(nib_over(w)), "r"(kMinus136));
+    asm("add.rn.bf16x2 %0, %1, %2;\n" : "=r"(d) : "r"(and_or(w, 0x000f000fu, 0x43004300u)), "r"(0xc308c308u));
     return d;
 }
 __device__ __forceinline__ uint32_t bf2_mul(uint32_t a, uint32_t b)
@@ -289,14 +290,9 @@ __device__ __forceinline__ void kv4_values(uint32_t half, int tile, const Kv4Lan
         uint32_t x = __byte_perm(wa[j / 2], wb[j / 2], sel), y = __byte_perm(wc[j / 2], wd[j / 2], sel);
 #pragma unroll
         for (int h = 0; h < 2; ++h, x >>= 8, y >>= 8) {
-            if (kF32) {
-                const uint32_t a0 = nib_bf16(x), a1 = nib_bf16(x >> 4), a2 = nib_bf16(y), a3 = nib_bf16(y >> 4);
-                mma_b16(acc[2 * j + h], a0, a1, a2, a3, b0, b1);
-                mma_b16(acc[2 * j + h], a0, a1, a2, a3, b2, b3);
-            } else {
-                mma_b16(acc[2 * j + h], nib_over(x), nib_over(x >> 4), nib_over(y), nib_over(y >> 4), b0, b1);
-                mma_b16(acc[2 * j + h], kMinus136, kMinus136, kMinus136, kMinus136, b0, b1);
-            }
+            const uint32_t a0 = nib_bf16(x), a1 = nib_bf16(x >> 4), a2 = nib_bf16(y), a3 = nib_bf16(y >> 4);
+            mma_b16(acc[2 * j + h], a0, a1, a2, a3, b0, b1);
+            if (kF32) mma_b16(acc[2 * j + h], a0, a1, a2, a3, b2, b3);
         }
     }
 }
@@ -310,7 +306,8 @@ __device__ __forceinline__ void kv4_mask(float (&sx)[4], int key, bool partial, 
     }
 }
 
-// What a warp knows of a row: of heads 2t and 2t + 1 the maximum, the sum of weights (this thread's keys) and the output.
+// What a warp knows of a row: of heads 2t and 2t + 1 what the weights are relative to (m, see kD4Grow; -inf before the first key), the
+// sum of weights (this thread's keys) and the output.
 template <int D>
 struct Kv4State {
     float m0, m1, l0, l1;
@@ -322,7 +319,7 @@ struct Kv4State {
 #pragma unroll
         for (int e = 0; e < D / 16; ++e) acc[e][0] = acc[e][1] = acc[e][2] = acc[e][3] = 0.f;
     }
-    // New logits have maxima mx0, mx1 (this thread's).  The maximum is moved only where it is exceeded by far.
+    // New logits have maxima mx0, mx1 (this thread's).
     __device__ __forceinline__ void raise(float mx0, float mx1, const Kv4Query<D> &q)
     {
         mx0 *= q.c0;
@@ -332,7 +329,9 @@ struct Kv4State {
             mx0 = fmaxf(mx0, __shfl_xor_sync(0xffffffffu, mx0, o));
             mx1 = fmaxf(mx1, __shfl_xor_sync(0xffffffffu, mx1, o));
         }
-        const bool up0 = mx0 > m0 + kD4Grow, up1 = mx1 > m1 + kD4Grow;
+        const bool up0 = mx0 > m0, up1 = mx1 > m1;
+        mx0 += kD4Grow;
+        mx1 += kD4Grow;
         if (__any_sync(0xffffffffu, up0 || up1)) {
             const float al0 = up0 ? ptx::ex2(m0 - mx0) : 1.f, al1 = up1 ? ptx::ex2(m1 - mx1) : 1.f;
             m0 = up0 ? mx0 : m0;

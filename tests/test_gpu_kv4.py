@@ -270,6 +270,50 @@ def test_decode_kv4_magnitudes(pa, oracle, k_scale, v_scale, q_scale):
     c.check(oracle, 8, 5, 1, q_scale=q_scale)
 
 
+@pytest.mark.parametrize("env", [{}, {"PA_DECODE_PATH": "cluster", "PA_DECODE_CLUSTER": "3"}, {"PA_DECODE_PATH": "persist"}])
+@pytest.mark.parametrize("hq,hkv,d", [(14, 2, 128), (4, 1, 64)])
+def test_decode_kv4_values_near_the_largest(pa, oracle, pa_env, hq, hkv, d, env):
+    """Values as large as their sum by the weights allows (its magnitudes stay below 3.02e38): finite, and right."""
+    pa_env(**env)
+    c = _Cache(pa, [1, 3, 64, 700, 3000], hkv, d, seed=22, k_scale=2.0)
+    for b, n in enumerate(c.lens):
+        i = torch.arange(n)
+        slots = (c.table[b].cpu()[i // 64].long() * 64 + i % 64).cuda()
+        g = torch.Generator().manual_seed(b)
+        v = torch.rand((n, hkv, d), generator=g).bfloat16().float()
+        v[torch.rand(v.shape, generator=g) < 0.1] *= -1
+        v[0, :, ::32] = 1.0
+        v = (v * (3e38 / n)).bfloat16().cuda()
+        pa.pa_kv4_append(pa.pa_kv4_read(c.pool, slots, d)[0], v, c.pool, slots)
+        c.k[b], c.v[b] = (x.double() for x in pa.pa_kv4_read(c.pool, slots, d, dtype=torch.float32))
+        assert torch.equal(c.v[b], plain.held(v))
+    for W, S in ((5, 1), (60, 1)):
+        c.check(oracle, hq, W, S, torch.float32)
+        c.check(oracle, hq, W, S)
+
+
+@pytest.mark.parametrize("env", [{}, {"PA_DECODE_PATH": "cluster", "PA_DECODE_CLUSTER": "1"}, {"PA_DECODE_PATH": "persist"}])
+@pytest.mark.parametrize("o_dtype", [torch.bfloat16, torch.float32])
+def test_decode_kv4_large_values_under_a_rising_maximum(pa, pa_env, env, o_dtype):
+    """16 blocks of keys, half of them with logits of 4, before or behind those of 0: exp(4) is a factor by which sums must not run
+    over where the weighted mean does not."""
+    pa_env(**env)
+    d, n = 64, 1024
+    c = _Cache(pa, [n, n], 1, d, seed=25)
+    v = torch.full((n, 1, d), 3e38 / 530, dtype=torch.bfloat16).cuda()     # (512 + 512 exp(-4) weights)
+    for b in range(2):
+        i = torch.arange(n)
+        slots = (c.table[b].cpu()[i // 64].long() * 64 + i % 64).cuda()
+        k = torch.zeros((n, 1, d))
+        k[(i >= 512) == (b == 0)] = 0.5
+        pa.pa_kv4_append(k.bfloat16().cuda(), v, c.pool, slots)
+        c.k[b], c.v[b] = plain.held(k.bfloat16().cuda()), plain.held(v)
+    q = torch.ones((2, 3, d), dtype=torch.bfloat16).cuda()                # logits of 32 / 8
+    o, lse, _ = pa.pa_decode_kv4(q, c.pool, c.table, c.lens_d, 60, 1, o_dtype=o_dtype)
+    for b in range(2):
+        _near(o[b], lse[b], plain.row_attention(q[b].double(), c.k[b][:, 0], c.v[b][:, 0], d ** -0.5), o_dtype)
+
+
 def test_decode_kv4_values_of_mixed_magnitude(pa, oracle):
     """A group of V a million times the others, keys whose V is zero, V zero everywhere, a single weight that counts."""
     c = _Cache(pa, [700, 300, 64], 1, 128, seed=10, k_scale=3.0)
