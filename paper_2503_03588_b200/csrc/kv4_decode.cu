@@ -9,8 +9,7 @@
 //
 // Logits take fp16 operands: q is bf16, and each head is multiplied by a power of two so that its largest entry lies in [2^10, 2^11)
 // and fits (entries below 2^-24 of it lose bits).  Weights are bf16, since V's scales may differ by any factor from key to key
-// and from group to group: rounded once as weights and once times a scale, half a step 2^-8 each, as the output's own
-// rounding; for fp32 outputs they come in two parts.
+// and from group to group, in two parts: one would be off by as much as the output's own rounding.
 //
 // The nibbles become 16-bit numbers without conversions.  K: w & 0x000f000f is two fp16 subnormals, u 2^-24, and w & 0x00f000f0 is
 // 16 times as much, for which the queries of the former are multiplied by 16; -8 sum_i q_i is what the accumulator starts
@@ -101,6 +100,19 @@ __device__ __forceinline__ uint32_t bf2_mul(uint32_t a, uint32_t b)
 {
     uint32_t d;
     asm("mul.rn.bf16x2 %0, %1, %2;\n" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
+// a b + c and a b - c, two at a time, rounded once.
+__device__ __forceinline__ uint32_t bf2_fma(uint32_t a, uint32_t b, uint32_t c)
+{
+    uint32_t d;
+    asm("fma.rn.bf16x2 %0, %1, %2, %3;\n" : "=r"(d) : "r"(a), "r"(b), "r"(c));
+    return d;
+}
+__device__ __forceinline__ uint32_t bf2_fms(uint32_t a, uint32_t b, uint32_t c)
+{
+    uint32_t d;
+    asm("{\n\t.reg .b32 n;\n\tneg.bf16x2 n, %3;\n\tfma.rn.bf16x2 %0, %1, %2, n;\n\t}\n" : "=r"(d) : "r"(a), "r"(b), "r"(c));
     return d;
 }
 __device__ __forceinline__ uint32_t cvt_f16x2(float lo, float hi)
@@ -235,8 +247,10 @@ __device__ __forceinline__ void kv4_logits(uint32_t half, int tile, const Kv4Lan
 
 // O^T += V^T P^T of the tile in V's half `half`: p are the weights of rows g, g + 8 and heads 2t, 2t + 1; of a partial block's
 // tile `keys` exist.  acc[2 j + h]: features 32 j + 4 g + 2 h + {0, 1}, heads 2t, 2t + 1.
-// The weights are transposed into the B operand as bf16 and then multiplied by the keys' scales of each group, two at a time:
-// two roundings, but a quarter of the conversions and transposes.  (fp32 outputs: scaled in fp32, group by group, two parts.)
+// Weights times scales come as two bf16 parts, so that they are off by 2^-14 at most (one part: 2^-7, more than the output's own
+// rounding).  For bf16 outputs the weights' two parts are transposed into the B operand once and multiplied by the keys' scales
+// there, two at a time: the first product is rounded, what that leaves is exact (8 x 8 bits less their upper 8) and goes into the
+// second one.  That is a quarter of the conversions and transposes.  fp32 outputs: scaled in fp32, group by group, off by 2^-16.
 template <int D, bool kF32>
 __device__ __forceinline__ void kv4_values(uint32_t half, int tile, const Kv4Lane<D> &at, const float (&p)[4], bool partial, int keys,
                                            float (&acc)[D / 16][4])
@@ -265,15 +279,18 @@ __device__ __forceinline__ void kv4_values(uint32_t half, int tile, const Kv4Lan
             if (!kF32 && at.key1 + 8 >= keys) sd[y] = 0u;
         }
     }
-    uint32_t t0 = 0u, t1 = 0u;
+    uint32_t t0 = 0u, t1 = 0u, t2 = 0u, t3 = 0u;
     if (!kF32) {
-        t0 = transpose8(ptx::cvt_bf16x2(p[0], p[1]));
-        t1 = transpose8(ptx::cvt_bf16x2(p[2], p[3]));
+        const uint32_t h0 = ptx::cvt_bf16x2(p[0], p[1]), h1 = ptx::cvt_bf16x2(p[2], p[3]);
+        t0 = transpose8(h0);
+        t1 = transpose8(h1);
+        t2 = transpose8(ptx::cvt_bf16x2(p[0] - bf16_lo(h0), p[1] - bf16_hi(h0)));
+        t3 = transpose8(ptx::cvt_bf16x2(p[2] - bf16_lo(h1), p[3] - bf16_hi(h1)));
     }
 #pragma unroll
     for (int j = 0; j < NG; ++j) {
         const uint32_t sel = j & 1 ? 0x7632u : 0x5410u;
-        uint32_t b0, b1, b2 = 0u, b3 = 0u;
+        uint32_t b0, b1, b2, b3;
         if (kF32) {
             const float s0 = j & 1 ? bf16_hi(sa[j / 2]) : bf16_lo(sa[j / 2]);
             const float s1 = j & 1 ? bf16_hi(sb[j / 2]) : bf16_lo(sb[j / 2]);
@@ -284,15 +301,18 @@ __device__ __forceinline__ void kv4_values(uint32_t half, int tile, const Kv4Lan
             b2 = transpose8(ptx::cvt_bf16x2(w0 - bf16_lo(h0), w1 - bf16_hi(h0)));  // what the rounding left
             b3 = transpose8(ptx::cvt_bf16x2(w2 - bf16_lo(h1), w3 - bf16_hi(h1)));
         } else {
-            b0 = bf2_mul(t0, __byte_perm(sa[j / 2], sb[j / 2], sel));
-            b1 = bf2_mul(t1, __byte_perm(sc[j / 2], sd[j / 2], sel));
+            const uint32_t s0 = __byte_perm(sa[j / 2], sb[j / 2], sel), s1 = __byte_perm(sc[j / 2], sd[j / 2], sel);
+            b0 = bf2_mul(t0, s0);
+            b1 = bf2_mul(t1, s1);
+            b2 = bf2_fma(t2, s0, bf2_fms(t0, s0, b0));
+            b3 = bf2_fma(t3, s1, bf2_fms(t1, s1, b1));
         }
         uint32_t x = __byte_perm(wa[j / 2], wb[j / 2], sel), y = __byte_perm(wc[j / 2], wd[j / 2], sel);
 #pragma unroll
         for (int h = 0; h < 2; ++h, x >>= 8, y >>= 8) {
             const uint32_t a0 = nib_bf16(x), a1 = nib_bf16(x >> 4), a2 = nib_bf16(y), a3 = nib_bf16(y >> 4);
             mma_b16(acc[2 * j + h], a0, a1, a2, a3, b0, b1);
-            if (kF32) mma_b16(acc[2 * j + h], a0, a1, a2, a3, b2, b3);
+            mma_b16(acc[2 * j + h], a0, a1, a2, a3, b2, b3);
         }
     }
 }

@@ -272,6 +272,27 @@ def test_decode_kv4_magnitudes(pa, oracle, k_scale, v_scale, q_scale):
 
 @pytest.mark.parametrize("env", [{}, {"PA_DECODE_PATH": "cluster", "PA_DECODE_CLUSTER": "3"}, {"PA_DECODE_PATH": "persist"}])
 @pytest.mark.parametrize("hq,hkv,d", [(14, 2, 128), (4, 1, 64)])
+def test_decode_kv4_weights_lose_less_than_the_output(pa, oracle, pa_env, hq, hkv, d, env):
+    """bf16 outputs are off by their own rounding, 2^-8 of them, and little else.  A weight in two bf16 parts is off by 2^-16, its
+    product with a scale once more by 2^-15 (the second part holds 2^-7 of it at most): below 2^-14 of the terms, and what the
+    logits' errors make of it (as in _near)."""
+    pa_env(**env)
+    c = _Cache(pa, [2, 9, 30, 64, 200, 1000], hkv, d, seed=26, k_scale=2.0)
+    q, o, lse, _ = c.check(oracle, hq, 5, 1)
+    for b, n in enumerate(c.lens):
+        j = torch.as_tensor(np.asarray(oracle.block_row((n - 1) // 64, 5, 1))).long()
+        i = (j[:, None] * 64 + torch.arange(64)).flatten()
+        i = i[i < n].cuda()
+        for h in range(hkv):
+            heads = slice(h * hq // hkv, (h + 1) * hq // hkv)
+            ref_o, _, size, most = plain.row_attention(q[b, heads].double(), c.k[b][i, h], c.v[b][i, h], d ** -0.5)
+            bound = ref_o.abs() * 2.0 ** -8 + (2 * (2.0 ** -18 * most + 2.0 ** -18) + 2.0 ** -14)[:, None] * size
+            err = (o[b, heads].double() - ref_o).abs()
+            assert (err <= bound).all(), float((err / bound).max())
+
+
+@pytest.mark.parametrize("env", [{}, {"PA_DECODE_PATH": "cluster", "PA_DECODE_CLUSTER": "3"}, {"PA_DECODE_PATH": "persist"}])
+@pytest.mark.parametrize("hq,hkv,d", [(14, 2, 128), (4, 1, 64)])
 def test_decode_kv4_values_near_the_largest(pa, oracle, pa_env, hq, hkv, d, env):
     """Values as large as their sum by the weights allows (its magnitudes stay below 3.02e38): finite, and right."""
     pa_env(**env)
