@@ -193,7 +193,7 @@ struct Kv4Query {
         top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
         // f is q 2^10 / 2^e with 2^e <= max |q| < 2^(e + 1) (q 2^14 / 2^e where the nibbles come as u 2^-24): products are u q 2^(-10 - e).
         const uint32_t field = min(max(top >> 7, 27u), 243u);  // e + 127 (heads below 2^-100 lose bits; up to 2^116 they fit)
-        const float down = __uint_as_float((264u - field) << 23), up = fmaxf(__uint_as_float((field + 10u) << 23) * scale_log2, 0x1p-126f);  // (above 0: times -inf it stays that)
+        const float down = __uint_as_float((264u - field) << 23), up = __uint_as_float((field + 10u) << 23) * scale_log2;
         c0 = __shfl_sync(0xffffffffu, up, 8 * t);
         c1 = __shfl_sync(0xffffffffu, up, 8 * t + 4);
 #pragma unroll
@@ -215,8 +215,9 @@ struct Kv4Query {
     }
 };
 
-// S^T = K Q^T of the tile at `k` (its first key's place in K's half; the scales lie `ks` behind the half's start): rows g and
-// g + 8 of heads 2t, 2t + 1, not yet times c0 and c1.
+// S^T = K Q^T of a tile of the half at `half`: rows g and g + 8 of heads 2t, 2t + 1, in powers of two.  Rounded here, once: the
+// largest logit of a row less itself is 0 then, however large (a fused product less the rounded maximum is off by half a step of
+// the logit, which from 2^30 on is more than the exponents of fp32 hold).
 template <int D>
 __device__ __forceinline__ void kv4_logits(uint32_t half, int tile, const Kv4Lane<D> &at, const Kv4Query<D> &q, float (&sx)[4])
 {
@@ -243,6 +244,10 @@ __device__ __forceinline__ void kv4_logits(uint32_t half, int tile, const Kv4Lan
         sx[2] = fmaf(s1, d[2], sx[2]);
         sx[3] = fmaf(s1, d[3], sx[3]);
     }
+    sx[0] = __fmul_rn(sx[0], q.c0);
+    sx[1] = __fmul_rn(sx[1], q.c1);
+    sx[2] = __fmul_rn(sx[2], q.c0);
+    sx[3] = __fmul_rn(sx[3], q.c1);
 }
 
 // O^T += V^T P^T of the tile in V's half `half`: p are the weights of rows g, g + 8 and heads 2t, 2t + 1; of a partial block's
@@ -340,10 +345,8 @@ struct Kv4State {
         for (int e = 0; e < D / 16; ++e) acc[e][0] = acc[e][1] = acc[e][2] = acc[e][3] = 0.f;
     }
     // New logits have maxima mx0, mx1 (this thread's).
-    __device__ __forceinline__ void raise(float mx0, float mx1, const Kv4Query<D> &q)
+    __device__ __forceinline__ void raise(float mx0, float mx1)
     {
-        mx0 *= q.c0;
-        mx1 *= q.c1;
 #pragma unroll
         for (int o = 4; o < 32; o *= 2) {
             mx0 = fmaxf(mx0, __shfl_xor_sync(0xffffffffu, mx0, o));
@@ -368,12 +371,12 @@ struct Kv4State {
         }
     }
     // The weights of logits sx, added to the sums; the tile's keys from `keys` on have none.
-    __device__ __forceinline__ void weigh(const float (&sx)[4], const Kv4Query<D> &q, int key, bool partial, int keys, float (&p)[4])
+    __device__ __forceinline__ void weigh(const float (&sx)[4], int key, bool partial, int keys, float (&p)[4])
     {
-        p[0] = ptx::ex2(fmaf(sx[0], q.c0, -m0));
-        p[1] = ptx::ex2(fmaf(sx[1], q.c1, -m1));
-        p[2] = ptx::ex2(fmaf(sx[2], q.c0, -m0));
-        p[3] = ptx::ex2(fmaf(sx[3], q.c1, -m1));
+        p[0] = ptx::ex2(sx[0] - m0);
+        p[1] = ptx::ex2(sx[1] - m1);
+        p[2] = ptx::ex2(sx[2] - m0);
+        p[3] = ptx::ex2(sx[3] - m1);
         if (partial) {
             if (key >= keys) p[0] = p[1] = 0.f;
             if (key + 8 >= keys) p[2] = p[3] = 0.f;
@@ -563,8 +566,8 @@ __global__ void __launch_bounds__(kC4Threads, 2) kv4_cluster_kernel(const Kv4Arg
                 float sx[4], p[4];
                 kv4_logits<D>(k_half, tile, at, q, sx);
                 kv4_mask(sx, at.key, partial, n_keys - 16 * tile);
-                st.raise(fmaxf(sx[0], sx[2]), fmaxf(sx[1], sx[3]), q);
-                st.weigh(sx, q, at.key, partial, n_keys - 16 * tile, p);
+                st.raise(fmaxf(sx[0], sx[2]), fmaxf(sx[1], sx[3]));
+                st.weigh(sx, at.key, partial, n_keys - 16 * tile, p);
                 kv4_values<D, kF32>(k_half + R4::kHalf, tile, at, p, partial, n_keys - 16 * tile, st.acc);
             }
             __syncwarp();
@@ -867,7 +870,7 @@ __global__ void __launch_bounds__(kR4Threads, 1) kv4_range_kernel(const Kv4Args 
             mx0 = fmaxf(mx0, fmaxf(sx[tile][0], sx[tile][2]));
             mx1 = fmaxf(mx1, fmaxf(sx[tile][1], sx[tile][3]));
         }
-        st.raise(mx0, mx1, q);
+        st.raise(mx0, mx1);
         wait_half(2);
         if (!ok) break;
         const uint32_t v_half = ring + slot * SM::kHalf;
@@ -875,7 +878,7 @@ __global__ void __launch_bounds__(kR4Threads, 1) kv4_range_kernel(const Kv4Args 
         for (int tile = 0; tile < 4; ++tile)
             if (!partial || 16 * tile < n_keys) {
                 float p[4];
-                st.weigh(sx[tile], q, at.key, partial, n_keys - 16 * tile, p);
+                st.weigh(sx[tile], at.key, partial, n_keys - 16 * tile, p);
                 kv4_values<D, kF32>(v_half, tile, at, p, partial, n_keys - 16 * tile, st.acc);
             }
         refill(2 * (x - first) + 1 + NH);

@@ -335,6 +335,39 @@ def test_decode_kv4_large_values_under_a_rising_maximum(pa, pa_env, env, o_dtype
         _near(o[b], lse[b], plain.row_attention(q[b].double(), c.k[b][:, 0], c.v[b][:, 0], d ** -0.5), o_dtype)
 
 
+@pytest.mark.parametrize("env", [{}, {"PA_DECODE_PATH": "cluster", "PA_DECODE_CLUSTER": "3"}, {"PA_DECODE_PATH": "persist"}])
+@pytest.mark.parametrize("q_scale,k_scale", [(1e5, 1e5), (1e9, 1e7), (1e20, 1e15)])
+@pytest.mark.parametrize("d", [64, 128])
+def test_decode_kv4_logits_beyond_the_range_of_exponents(pa, pa_env, d, q_scale, k_scale, env):
+    """Logits of 1e10 and of 1e35 lie so far apart that the largest takes all: its key's values, and it, whatever a step of fp32 is
+    there.  (fp32 sums are off by 2^-18 of the products' magnitudes at most, as in _near; a single weight is 1 or two parts of
+    it, so its value is exact to 2^-15.)"""
+    pa_env(**env)
+    c = _Cache(pa, [1, 250, 700], 2, d, seed=27, k_scale=k_scale)
+    q = _randn(3, 10, d, seed=28, scale=q_scale).cuda()
+    for o_dtype in (torch.float32, torch.bfloat16):
+        o, lse, ws = pa.pa_decode_kv4(q, c.pool, c.table, c.lens_d, 60, 1, o_dtype=o_dtype)
+        pa.pa_decode_status(ws)
+        assert torch.isfinite(o.float()).all() and torch.isfinite(lse).all()
+        taken = 0
+        for b in range(3):
+            for h in range(2):
+                heads = slice(5 * h, 5 * h + 5)
+                logits = q[b, heads].double() @ c.k[b][:, h].T * d ** -0.5
+                off = 2.0 ** -18 * plain.row_attention(q[b, heads].double(), c.k[b][:, h], c.v[b][:, h], d ** -0.5)[3]
+                first = logits.max(-1).values
+                assert ((lse[b, heads].double() - first).abs() <= off + first.abs() * 2.0 ** -22).all()
+                for g in range(5):
+                    rivals = (logits[g] > first[g] - 2 * off[g] - 200).sum()
+                    if rivals > 1:
+                        continue
+                    taken += 1
+                    v = c.v[b][int(logits[g].argmax()), h]
+                    err = (o[b, 5 * h + g].double() - v).abs()
+                    assert (err <= v.abs() * (2.0 ** -7 if o_dtype == torch.bfloat16 else 2.0 ** -15)).all()
+        assert taken >= 25
+
+
 def test_decode_kv4_values_of_mixed_magnitude(pa, oracle):
     """A group of V a million times the others, keys whose V is zero, V zero everywhere, a single weight that counts."""
     c = _Cache(pa, [700, 300, 64], 1, 128, seed=10, k_scale=3.0)
