@@ -172,9 +172,11 @@ struct Kv4Lane {
 template <int D>
 struct Kv4Query {
     static constexpr int NG = D / 32;
+    static constexpr uint32_t kMore = 1u << 31;  // (in `more` of every lane, if any head of the warp has some)
     uint32_t f[NG][4];
     float o0[NG], o1[NG];  // of heads 2t and 2t + 1: -8 times the sum of the group's features, as the products come (2^-20)
     float c0, c1;          // of the same heads: the powers of two, the softmax scale, log2 e
+    uint32_t more;         // of the same heads (halves): exponents that c0, c1 have no room for; 0 but for heads from 2^117 on
     static __device__ __forceinline__ void load(const Kv4Args &a, uint32_t row, int lane, uint4 (&raw)[NG])
     {
         const int g = lane >> 2, t = lane & 3;
@@ -192,10 +194,12 @@ struct Kv4Query {
         top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
         top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
         // f is q 2^10 / 2^e with 2^e <= max |q| < 2^(e + 1) (q 2^14 / 2^e where the nibbles come as u 2^-24): products are u q 2^(-10 - e).
-        const uint32_t field = min(max(top >> 7, 27u), 243u);  // e + 127 (heads below 2^-100 lose bits; up to 2^116 they fit)
-        const float down = __uint_as_float((264u - field) << 23), up = __uint_as_float((field + 10u) << 23) * scale_log2;
+        const uint32_t field = min(max(top >> 7, 27u), 254u), fits = min(field, 243u);  // e + 127 (heads below 2^-100 lose bits)
+        const float down = __uint_as_float((264u - field) << 23), up = __uint_as_float((fits + 10u) << 23) * scale_log2;
         c0 = __shfl_sync(0xffffffffu, up, 8 * t);
         c1 = __shfl_sync(0xffffffffu, up, 8 * t + 4);
+        more = __any_sync(0xffffffffu, field > fits) ? __byte_perm(__shfl_sync(0xffffffffu, field - fits, 8 * t),
+                                                                   __shfl_sync(0xffffffffu, field - fits, 8 * t + 4), 0x5410) | kMore : 0u;
 #pragma unroll
         for (int j = 0; j < NG; ++j) {
             f[j][0] = cvt_f16x2(bf16_lo(raw[j].x) * (16.f * down), bf16_lo(raw[j].z) * (16.f * down));
@@ -243,6 +247,13 @@ __device__ __forceinline__ void kv4_logits(uint32_t half, int tile, const Kv4Lan
         sx[1] = fmaf(s0, d[1], sx[1]);
         sx[2] = fmaf(s1, d[2], sx[2]);
         sx[3] = fmaf(s1, d[3], sx[3]);
+    }
+    if (q.more) {  // (all lanes or none)
+        const float x0 = __uint_as_float((127u + (q.more & 0xffu)) << 23), x1 = __uint_as_float((127u + (q.more >> 16 & 0xffu)) << 23);
+        sx[0] *= x0;
+        sx[1] *= x1;
+        sx[2] *= x0;
+        sx[3] *= x1;
     }
     sx[0] = __fmul_rn(sx[0], q.c0);
     sx[1] = __fmul_rn(sx[1], q.c1);

@@ -368,6 +368,46 @@ def test_decode_kv4_logits_beyond_the_range_of_exponents(pa, pa_env, d, q_scale,
         assert taken >= 25
 
 
+@pytest.mark.parametrize("env", [{}, {"PA_DECODE_PATH": "cluster", "PA_DECODE_CLUSTER": "3"}, {"PA_DECODE_PATH": "persist"}])
+@pytest.mark.parametrize("d", [64, 128])
+def test_decode_kv4_queries_near_the_largest(pa, pa_env, d, env):
+    """Heads of up to 3e38 beside ones of 1 and of 1e-30: over keys of zeros every head gives the mean of V, over keys of 2^-97 the
+    large heads' logits are some 2^30, far apart, and the one key with the largest takes all (their fp32 sums are off by 2^-18 of
+    the products' magnitudes at most, as in _near)."""
+    pa_env(**env)
+    c = _Cache(pa, [300, 250, 64], 1, d, seed=23)
+    for b, scale in enumerate((0.0, 2.0 ** -97, 2.0 ** -97)):
+        n = c.lens[b]
+        i = torch.arange(n)
+        slots = (c.table[b].cpu()[i // 64].long() * 64 + i % 64).cuda()
+        k, v = _randn(n, 1, d, seed=40 + b, scale=scale).cuda(), _randn(n, 1, d, seed=50 + b).cuda()
+        pa.pa_kv4_append(k, v, c.pool, slots)
+        c.k[b], c.v[b] = plain.held(k), plain.held(v)
+    q = torch.rand((3, 5, d), generator=torch.Generator().manual_seed(24)) * 2 - 1
+    q *= torch.tensor([3e38, 1.0, 2.0 ** 118, 1e-30, 1e35])[None, :, None]
+    q[:, :, 5] = torch.tensor([3.3e38, 1.0, 2.0 ** 118, 1e-30, 1e35])
+    q = q.bfloat16().cuda()
+    for o_dtype in (torch.float32, torch.bfloat16):
+        o, lse, ws = pa.pa_decode_kv4(q, c.pool, c.table, c.lens_d, 5, 1, o_dtype=o_dtype)
+        pa.pa_decode_status(ws)
+        assert torch.isfinite(o.float()).all() and torch.isfinite(lse).all()
+        for b in range(3):
+            ref = plain.row_attention(q[b].double(), c.k[b][:, 0], c.v[b][:, 0], d ** -0.5)
+            small = torch.tensor([1, 3]).cuda() if b else torch.arange(5).cuda()
+            _near(o[b, small], lse[b, small], [x[small] for x in ref], o_dtype)
+            if b == 0:
+                continue
+            logits = q[b].double() @ c.k[b][:, 0].T * d ** -0.5
+            for h in (0, 2, 4):
+                first, second = logits[h].topk(2).values.tolist()
+                off = 2.0 ** -18 * float(ref[3][h])
+                assert first - second > 2 * off + 200           # (the inputs are such)
+                assert abs(float(lse[b, h]) - first) <= off + abs(first) * 2.0 ** -22
+                err = (o[b, h].double() - c.v[b][int(logits[h].argmax()), 0]).abs()
+                bound = 2.0 ** -8 if o_dtype == torch.bfloat16 else 2.0 ** -15
+                assert (err <= 2 * bound * c.v[b][int(logits[h].argmax()), 0].abs()).all()
+
+
 def test_decode_kv4_values_of_mixed_magnitude(pa, oracle):
     """A group of V a million times the others, keys whose V is zero, V zero everywhere, a single weight that counts."""
     c = _Cache(pa, [700, 300, 64], 1, 128, seed=10, k_scale=3.0)
