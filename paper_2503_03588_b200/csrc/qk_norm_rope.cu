@@ -421,9 +421,11 @@ __global__ void __launch_bounds__(kBackThreads, 2) rope_backward_kernel(const Ro
                 d += stride * sd.head;
             };
             load(first);
-            const Eight w = load_weights<kPairs>(which ? a.k_weight : a.q_weight, a.w_f32, p);
-            if (!looked_up) {
-                t = load_angles<kPairs>(a, p, there ? pos : 0);
+            // (A token without a position has weights and angles of zero: what these are, finite or not, is nothing to it.)
+            Eight w = {};
+            if (there) w = load_weights<kPairs>(which ? a.k_weight : a.q_weight, a.w_f32, p);
+            if (there && !looked_up) {
+                t = load_angles<kPairs>(a, p, pos);
                 looked_up = true;
             }
             for (int h = first; h < H; h += stride) {

@@ -201,6 +201,29 @@ def test_norm_rope_leaves_tokens_without_a_position_alone(pa, tokens):
         assert ((grads[2 + i].double() - dw).abs() <= dws * 2.0 ** -14).all()
 
 
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("tokens", [6, 1300])
+def test_gradients_of_tokens_without_a_position_are_zero_whatever_weights_and_angles_are(pa, tokens, interleaved):
+    """Infinite and NaN weights; a row of the table that no token is at holds NaN and infinities."""
+    hq, hkv, d = 5, 1, 128
+    q, k, wq, wk, cs, pos = _inputs(tokens, hq, hkv, d, 64, 14)
+    pos.clamp_(min=1)
+    bad = torch.zeros(tokens, dtype=torch.bool).cuda()
+    bad[::3], bad[-1] = True, True
+    pos[bad] = -1
+    back = [torch.randn((tokens, h, d)).cuda() for h in (hq, hkv)]
+    ref = pa.pa_qk_norm_rope_backward(q, k, wq, wk, cs, pos, *back, interleaved=interleaved)
+    cs[0, ::2], cs[0, 1::2] = float("nan"), float("inf")
+    got = pa.pa_qk_norm_rope_backward(q, k, wq, wk, cs, pos, *back, interleaved=interleaved)
+    for a, b in zip(got[:4], ref):
+        assert torch.equal(a, b)
+    wq[3], wk[70], wk[127] = float("inf"), float("nan"), float("-inf")
+    got = pa.pa_qk_norm_rope_backward(q, k, wq, wk, cs, pos, *back, interleaved=interleaved)
+    assert (got[0][bad] == 0).all() and (got[1][bad] == 0).all()
+    for a, b in zip(got[2:4], ref[2:4]):      # (the weights' gradients do not depend on the weights)
+        assert torch.equal(a, b)
+
+
 def test_norm_rope_strides_batches_and_in_place(pa):
     """[batch, N, H, D] views with gaps, a head axis inside out, expanded inputs, outputs over the inputs."""
     b, n, hq, hkv, d = 2, 33, 4, 2, 128
