@@ -408,6 +408,7 @@ typedef struct {
 } pa_rope_params;
 
 /* q, k, q_out, k_out: device bf16 by strides; q_out may be q and k_out may be k, with the same strides.
+ * Two heads of an output must not share a number (PA_ERR_SHAPE, whichever strides have them do so).
  * q_weight, k_weight: device, w_dtype [head_dim].  cos_sin: device fp32 [max_positions, rotary_dim].
  * positions: device int32 [batch, seq_len].  One kernel is enqueued. */
 pa_status pa_qk_norm_rope(const pa_rope_params *p, const void *q, const void *k, const void *q_weight,

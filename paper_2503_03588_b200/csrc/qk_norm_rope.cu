@@ -13,6 +13,7 @@
 #include <cuda_bf16.h>
 #include <math.h>
 
+#include <algorithm>
 #include <type_traits>
 
 #include "common.cuh"
@@ -543,16 +544,50 @@ static pa_status check_rope(const pa_rope_params *p)
     return PA_OK;
 }
 
-// Writing through a stride of 0, or one below a head, would have rows overlap.
+// Whether two heads of a tensor share a number.  Axes of one entry have no part in it.
+static bool rows_overlap(const pa_strides &st, const int64_t (&sizes)[3], int64_t D)
+{
+    struct Axis {
+        int64_t size, stride;
+    } x[3];
+    int n = 0;
+    for (int i = 0; i < 3; ++i)
+        if (sizes[i] > 1) x[n++] = {sizes[i], i == 0 ? st.batch : i == 1 ? st.seq : st.head};
+    // No, if each axis steps over all that the axes of smaller strides cover: nearly every tensor.
+    std::sort(x, x + n, [](const Axis &a, const Axis &b) { return a.stride < b.stride; });
+    bool nested = true;
+    int64_t covered = D;
+    for (int i = 0; i < n && nested; ++i) {
+        nested = x[i].stride >= covered && x[i].stride <= (INT64_MAX - covered) / x[i].size;
+        covered += x[i].stride * (nested ? x[i].size - 1 : 0);
+    }
+    if (nested) return false;
+    for (int i = 0; i < n; ++i)
+        if (x[i].stride < D || x[i].stride > INT64_MAX / 4 / x[i].size) return true;  // (the latter: beyond any memory)
+    // Else heads overlap where steps a and b along two axes lie less than a head from a step c along the third: all a and b of the
+    // two shorter axes are tried.  (Where these are more than 2^16, the tensor is refused.)
+    std::sort(x, x + n, [](const Axis &a, const Axis &b) { return a.size < b.size; });
+    while (n < 3) x[n++] = {1, 0};
+    std::sort(x, x + n, [](const Axis &a, const Axis &b) { return a.size < b.size; });
+    if (x[0].size > (1 << 16) / x[1].size) return true;
+    for (int64_t a = 0; a < x[0].size; ++a)
+        for (int64_t b = a ? 1 - x[1].size : 0; b < x[1].size; ++b) {
+            const int64_t at = a * x[0].stride + b * x[1].stride, away = at < 0 ? -at : at;
+            const int64_t c = away / x[2].stride;  // (c and c + 1 steps are the nearest ones)
+            for (int64_t y = c; y <= c + 1 && y < x[2].size; ++y) {
+                const int64_t d = away - y * x[2].stride;
+                if ((a || b || y) && d < D && -d < D) return true;
+            }
+        }
+    return false;
+}
+
+// Rows that are written must not lie over one another.
 static pa_status check_written(const pa_rope_params *p)
 {
-    const pa_strides *st[2] = {&p->q_out, &p->k_out};
-    const int32_t heads[2] = {p->n_q_heads, p->n_kv_heads};
-    for (int i = 0; i < 2; ++i) {
-        if ((heads[i] > 1 && st[i]->head < p->head_dim) || (p->seq_len > 1 && st[i]->seq < p->head_dim) ||
-            (p->batch > 1 && st[i]->batch < p->head_dim))
-            return fail(PA_ERR_SHAPE, "rows of the outputs overlap");
-    }
+    const int64_t q[3] = {p->batch, p->seq_len, p->n_q_heads}, k[3] = {p->batch, p->seq_len, p->n_kv_heads};
+    if (rows_overlap(p->q_out, q, p->head_dim) || rows_overlap(p->k_out, k, p->head_dim))
+        return fail(PA_ERR_SHAPE, "rows of the outputs overlap");
     return PA_OK;
 }
 

@@ -1,5 +1,6 @@
 """Refusals of the calls around the attention (tables, norms with rotation, 4-bit cache): before anything is launched."""
 import ctypes
+import random
 
 import pytest
 import torch
@@ -91,6 +92,38 @@ def test_rope_refusals(b):
     assert backward(_changed(good), ws=0) == backward(_changed(good), ws_bytes=100) == "PA_ERR_WORKSPACE"
     assert backward(_changed(good), ws=P + 4) == "PA_ERR_ALIGNMENT"
     assert b.lib.pa_qk_norm_rope_backward_workspace_bytes(_changed(good)) == 25 * 2 * 128 * 4   # CTAs of eight warps, two warps a token
+
+
+def test_rope_refuses_outputs_whose_rows_overlap(b):
+    """Heads that share a number, whichever axes' strides have them do so; heads that interleave without sharing any are none of
+    these.  (A null array stops the calls that are not refused: it is looked at next.)"""
+    s, o = b.pa_strides(0, 512, 128), b.pa_strides(1 << 20, 512, 128)
+
+    def status(out, which="q_out", **kv):
+        good = b.pa_rope_params(1, 4, 2, 128, 100, 128, 0, 100, 1e-6, b.PA_BF16, s, s, o, o)
+        args = [0] + [P] * 7
+        return b.pa_status_string(b.lib.pa_qk_norm_rope(_changed(good, **{which: b.pa_strides(*out)}, **kv), *args, NULL))
+
+    assert status((1 << 20, 512, 128)) == status((0, 512, 128)) == "PA_ERR_INVALID_ARG"        # (one batch entry: its stride is not used)
+    for out in ((0, 128, 128), (0, 384, 128), (0, 128, 12672), (0, 256, 97 * 256)):   # head h + 1 of a token is head h of another
+        assert status(out) == "PA_ERR_SHAPE", out
+    for out in ((128, 512, 128), (51072, 512, 128), (512, 512, 128)):
+        assert status(out, batch=2) == "PA_ERR_SHAPE", out
+    assert status((0, 128, 128), "k_out") == status((512, 512, 128), "k_out", batch=2) == "PA_ERR_SHAPE"
+    assert status((51200, 512, 128), batch=2) == status((512, 1024, 128), batch=2) == status((512, 1024, 128), "k_out", batch=2, n_kv_heads=4) == "PA_ERR_INVALID_ARG"
+    assert status((0, 128, 12800)) == status((0, 256, 128), n_q_heads=2) == status((0, 256, 97 * 256 + 128)) == "PA_ERR_INVALID_ARG"   # (between others)
+    assert status((1 << 62, 1 << 62, 1 << 62), batch=2) == "PA_ERR_SHAPE"                       # (nor beyond 64 bits)
+    rng = random.Random(5)
+    seen = {True: 0, False: 0}
+    for _ in range(4000):
+        sizes = [rng.randint(1, 3), rng.randint(1, 5), rng.randint(1, 4)]
+        strides = [8 * rng.randint(0, 60 if rng.random() < 0.5 else 20) for _ in sizes]
+        at = sorted(x * strides[0] + y * strides[1] + z * strides[2] for x in range(sizes[0]) for y in range(sizes[1]) for z in range(sizes[2]))
+        overlap = any(v - u < 64 for u, v in zip(at, at[1:]))
+        seen[overlap] += 1
+        got = status(strides, batch=sizes[0], seq_len=sizes[1], n_q_heads=sizes[2], head_dim=64, rotary_dim=64)
+        assert got == ("PA_ERR_SHAPE" if overlap else "PA_ERR_INVALID_ARG"), (sizes, strides)
+    assert min(seen.values()) > 500
 
 
 def test_kv4_refusals(b):
