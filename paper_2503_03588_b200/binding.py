@@ -404,7 +404,8 @@ def pa_build_block_tables(new_lens, cache_lens, free_pages, free_count, block_ta
     tensors [batch], a stack of free pages and its height free_count [1], block_table int32 [batch, max_blocks]
     (its new entries are written).  lens_out may be cache_lens and free_left may be free_count.
     Returns (cu_seqlens int32 [batch + 1], slot_map int64 [max_tokens], positions int32 [max_tokens], lens_out,
-    free_left, workspace)."""
+    free_left, workspace).  Here and in the calls below, results of up to 64 KB each that are allocated here share one
+    storage: clone what is saved or resized."""
     return _calls.build_block_tables(new_lens, cache_lens, free_pages, free_count, block_table, n_pages, max_tokens,
                                      cu_seqlens, slot_map, positions, lens_out, free_left, workspace, block)
 

@@ -349,9 +349,10 @@ void on_current_device(const T &...tensors)
     expect(on, "expected tensors on the current CUDA device");
 }
 
-// The outputs that a call's caller has not given.  Small ones share one allocation: a call that takes the GPU 2 us spent 7 us of
-// host time on six of them.
+// The outputs that a call's caller has not given.  Those of up to kShare bytes share one allocation: a call that takes the GPU 2 us
+// spent 7 us of host time on six of them.  Larger ones have their own, so that who keeps a small one keeps little else.
 class Fresh {
+    static constexpr int64_t kShare = 64 << 10;
     struct One {
         at::IntArrayRef size;
         at::ScalarType type;
@@ -359,24 +360,24 @@ class Fresh {
     };
     const at::Tensor &like;
     at::Tensor base;
-    int64_t most, total = 0;
+    int64_t total = 0;  // of the shared ones
     c10::SmallVector<One, 8> list;
 
 public:
-    explicit Fresh(const at::Tensor &t, int64_t bytes = 1 << 20) : like(t), most(bytes) {}
+    explicit Fresh(const at::Tensor &t) : like(t) {}
     // An output that will be needed if `given` is None.  (`size` has to outlive this.)
     void add(PyObject *given, at::IntArrayRef size, at::ScalarType type)
     {
         int64_t n = given == Py_None ? (int64_t)c10::elementSize(type) : 0;
         for (const int64_t x : size) n *= x;
         list.push_back({size, type, total, n});
-        total += (n + 255) / 256 * 256;
+        if (n <= kShare) total += (n + 255) / 256 * 256;
     }
     Out operator()(size_t i, PyObject *given)
     {
         const One &o = list[i];
         return Out(given, [&]() -> at::Tensor {
-            if (total > most) return make(like, o.size, o.type);
+            if (o.bytes > kShare) return make(like, o.size, o.type);
             if (!base.defined()) base = make(like, {total}, at::kByte);
             at::Tensor t = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(base.storage()), base.key_set(), c10::scalarTypeToTypeMeta(o.type));
             t.unsafeGetTensorImpl()->set_sizes_contiguous(o.size);
@@ -409,7 +410,7 @@ PyObject *build_block_tables(PyObject *const *x)
     const pa_table_params p = {(int32_t)batch, block, (int32_t)table.size(1), n_pages, max_tokens,
                                (int32_t)pages.numel()};
     const int64_t some = batch + 1, tokens = max_tokens, one = 1, bytes = (int64_t)pa_build_block_tables_workspace_bytes(&p) + 16;
-    Fresh outs(fresh, 64 << 20);
+    Fresh outs(fresh);
     outs.add(x[7], some, at::kInt);
     outs.add(x[8], tokens, at::kLong);
     outs.add(x[9], tokens, at::kInt);

@@ -105,6 +105,27 @@ def test_tables_captured_and_replayed(pa):
     np.testing.assert_array_equal(t.cpu().numpy(), ref[2])
 
 
+def test_small_results_do_not_hold_large_ones(pa):
+    """Who keeps the stack's height, the lengths or a weight's gradient keeps no slots, no workspace and no other gradients with
+    it: large results have storages of their own, the small ones' is small."""
+    t, free = _ints(np.full((300, 40), -1)), _ints(np.arange(12000))
+    cu, slots, positions, lens, left, ws = pa.pa_build_block_tables(_ints([2000] * 300), _ints([5] * 300), free, _ints([12000]), t, 12000, 600000)
+    assert int(left) == 12000 - 300 * 31       # 2005 tokens are 32 pages, one of which each has
+    small = {x.untyped_storage().data_ptr() for x in (cu, lens, left, ws)}
+    for x in (cu, lens, left, ws):
+        assert x.untyped_storage().nbytes() <= 6 * 65536
+    for x in (slots, positions):
+        assert x.untyped_storage().nbytes() == x.numel() * x.element_size() and x.untyped_storage().data_ptr() not in small
+    args = _inputs(200, 8, 2, 128, 128, 15)
+    grads = pa.pa_qk_norm_rope_backward(*args, *(torch.randn((200, h, 128)).cuda() for h in (8, 2)))
+    assert grads[0].untyped_storage().nbytes() == grads[0].numel() * 2      # 400 KB
+    assert grads[2].untyped_storage().nbytes() <= 5 * 65536
+    for a, b in ((0, 1), (0, 2), (0, 4)):
+        assert grads[a].untyped_storage().data_ptr() != grads[b].untyped_storage().data_ptr()
+    out = pa.pa_qk_norm_rope(*args)
+    assert out[0].untyped_storage().nbytes() == out[0].numel() * 2
+
+
 def test_tables_arrays_off_16_bytes(pa):
     """Slots and positions that start on an odd entry."""
     slots, positions = torch.full((200,), 7, dtype=torch.int64).cuda(), torch.full((200,), 7, dtype=torch.int32).cuda()
