@@ -446,8 +446,11 @@ def pa_kv4_read(kv_pool, slot_map, head_dim: int, k_out=None, v_out=None, dtype=
 
 def kv4_params(q, kv_pool, block_table, window_blocks: int, sink_blocks: int, softmax_scale: float = 0.0,
                o_dtype=torch.bfloat16) -> pa_kv4_params:
+    """What pa_decode_kv4_workspace_bytes takes: q [batch, Hq, D]; kv_pool uint8 [n_pages, Hkv, bytes]; block_table [batch,
+    max_blocks].  As in the call itself, the stride of an axis of one entry is not looked at."""
     batch, hq, d = q.shape
-    pool = pa_kv4_pool(kv_pool.shape[1], d, 64, kv_pool.shape[0], kv_pool.stride(0), kv_pool.stride(1))
+    strides = [kv_pool.stride(i) if kv_pool.shape[i] > 1 else 0 for i in range(2)]
+    pool = pa_kv4_pool(kv_pool.shape[1], d, 64, kv_pool.shape[0], *strides)
     return pa_kv4_params(batch, hq, window_blocks, sink_blocks, block_table.shape[1], float(softmax_scale),
                          PA_F32 if o_dtype == torch.float32 else PA_BF16, pool)
 

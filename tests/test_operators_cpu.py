@@ -193,6 +193,21 @@ def test_decode_kv4_refusals(b):
     assert status(_changed(good), ws=P + 4) == "PA_ERR_ALIGNMENT"
 
 
+def test_decode_kv4_workspace_from_tensors(b):
+    """The size for what the call takes, pools whose axes of one entry have odd strides among them."""
+    q, table = torch.zeros((2, 28, 128), dtype=torch.bfloat16), torch.zeros((2, 64), dtype=torch.int32)
+    want = 256 + 148 * 2 * (4 + 8 * 130) * 4
+    buf = torch.zeros(64 * 9216, dtype=torch.uint8)
+    for pool in (buf.view(16, 4, 9216), buf.view(8, 8, 9216)[:, :4], buf.as_strided((1, 4, 9216), (5, 9216, 1)),
+                 buf.as_strided((16, 1, 9216), (9216, 7, 1)), buf.as_strided((1, 1, 9216), (1, 3, 1))):
+        heads = 28 // pool.shape[1]
+        params = b.kv4_params(q if heads <= 8 else q[:, :8], pool, table, 5, 1)
+        assert b.pa_decode_kv4_workspace_bytes(params) == want, pool.stride()
+        assert params.n_q_heads == (28 if heads <= 8 else 8) and params.o_dtype == b.PA_BF16
+    assert b.pa_decode_kv4_workspace_bytes(b.kv4_params(q, buf.view(16, 4, 9216)[:, :3], table, 5, 1)) == 0     # 28 heads on 3
+    assert b.kv4_params(q, buf.view(16, 4, 9216), table, 5, 1, 0.5, torch.float32).o_dtype == b.PA_F32
+
+
 def test_tensors_that_do_not_fit_are_refused(b):
     """From Python: types, shapes, strides, devices (there is nothing on a GPU here)."""
     bf = lambda *s: torch.zeros(s, dtype=torch.bfloat16)  # noqa: E731
