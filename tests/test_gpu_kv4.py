@@ -94,6 +94,24 @@ def test_every_quotient_of_two_mantissas(pa):
     assert torch.equal(k.double(), plain.held(x)) and torch.equal(v, -k)
 
 
+def test_every_quotient_with_no_numerator_left_out(pa):
+    """All 128 mantissas of a number against all 128 of its group's largest, 0 to 4 octaves below it: 16 numbers and the largest a
+    group, eight groups in two heads."""
+    vals = torch.arange(128, 256).float()
+    x = torch.zeros((5, 128, 2, 4, 32))
+    for e in range(5):
+        for i in range(128):
+            x[e, i, :, :, :16] = (vals * 2.0 ** -e).clamp(max=float(vals[i])).reshape(2, 4, 16)
+    x[..., 31] = vals[None, :, None, None]
+    x = x.reshape(640, 2, 128).bfloat16().cuda()
+    below = x.view(5, 128, 8, 32)[1:, :, :, :16].reshape(4, 128, 128)
+    assert torch.equal(below[3].double() * 16, vals.double().cuda().expand(128, 128))   # (none has been replaced)
+    pool, slots = _pool(pa, 10, 2, 128), torch.arange(640).cuda()
+    pa.pa_kv4_append(x, -x, pool, slots)
+    k, v = pa.pa_kv4_read(pool, slots, 128, dtype=torch.float32)
+    assert torch.equal(k.double(), plain.held(x)) and torch.equal(v, -k)
+
+
 def test_append_strided_pool_and_tensors(pa):
     """A layer's part of a pool of all layers; heads that lie far apart; expanded values; no tokens at all."""
     d, heads = 64, 3
@@ -534,6 +552,40 @@ def test_decode_kv4_on_two_streams_at_once(pa):
     for i, (o, lse, ws) in got:
         assert torch.equal(o, ref[i][0]) and torch.equal(lse, ref[i][1])
         pa.pa_decode_status(ws)
+
+
+def test_appends_reads_and_decodes_on_two_streams_at_once(pa):
+    """Two caches on two streams: new tokens in, read back and decoded over, step after step, with nothing in between."""
+    caches = [_Cache(pa, [1000 + 90 * i + 7 * s for i in range(30)], 4, 128, seed=30 + s) for s in range(2)]
+    q = _randn(30, 28, 128).cuda()
+    new = [[_randn(30, 4, 128, seed=60 + 10 * s + i).cuda() for i in range(10)] for s in range(2)]
+
+    def steps(s):
+        c, out = caches[s], []
+        lens = c.lens_d.clone()
+        pages = torch.arange(30).cuda()
+        for i in range(10):
+            slots = c.table[pages, (lens.long() - 1 - i) // 64].long() * 64 + (lens.long() - 1 - i) % 64   # (over the last tokens)
+            pa.pa_kv4_append(new[s][i], new[s][9 - i], c.pool, slots)
+            out += [*pa.pa_kv4_read(c.pool, slots, 128), *pa.pa_decode_kv4(q, c.pool, c.table, lens, 5, 1)[:2]]
+        return out
+
+    before = [c.pool.clone() for c in caches]
+    ref = [steps(s) for s in range(2)]
+    streams, got = [torch.cuda.Stream() for _ in range(2)], []
+    torch.cuda.synchronize()
+    for _ in range(8):
+        for s, stream in enumerate(streams):
+            with torch.cuda.stream(stream):
+                caches[s].pool.copy_(before[s])
+                got.append((s, steps(s)))
+    torch.cuda.synchronize()
+    for s, outs in got:
+        for a, b in zip(outs, ref[s]):
+            assert torch.equal(a, b)
+    k = [plain.held(x) for x in new[0]]
+    for i in range(10):
+        assert torch.equal(ref[0][4 * i].double(), k[i].float().bfloat16().double())
 
 
 # ------------------------------------------------------------------ together
