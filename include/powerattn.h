@@ -481,7 +481,7 @@ size_t pa_decode_kv4_workspace_bytes(const pa_kv4_params *p);
 
 /* As pa_decode_paged (the same row of the mask, block_table, cache_lens, outputs, and pa_decode_status on the
  * workspace), on a 4-bit pool.  Logits are sums of exact products in fp32.  The weights, times V's scales, are
- * held in two bf16 parts.
+ * held in two bf16 parts, for fp32 outputs in three.
  * Outputs are finite where the values' magnitudes, summed by the weights exp(S - max S), stay below fp32's largest.
  * workspace: device, 16-byte aligned, >= pa_decode_kv4_workspace_bytes(p); calls that share one must not
  * overlap on the GPU.  A table entry outside [0, n_pages) is clamped into the pool; the sequence's result is

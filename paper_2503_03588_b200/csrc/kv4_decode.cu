@@ -9,7 +9,7 @@
 //
 // Logits take fp16 operands: q is bf16, and each head is multiplied by a power of two so that its largest entry lies in [2^10, 2^11)
 // and fits (entries below 2^-24 of it lose bits).  Weights are bf16, since V's scales may differ by any factor from key to key
-// and from group to group, in two parts: one would be off by as much as the output's own rounding.
+// and from group to group, in two parts (one would be off by as much as the output's own rounding), for fp32 outputs in three.
 //
 // The nibbles become 16-bit numbers without conversions.  K: w & 0x000f000f is two fp16 subnormals, u 2^-24, and w & 0x00f000f0 is
 // 16 times as much, for which the queries of the former are multiplied by 16; -8 sum_i q_i is what the accumulator starts
@@ -266,7 +266,8 @@ __device__ __forceinline__ void kv4_logits(uint32_t half, int tile, const Kv4Lan
 // Weights times scales come as two bf16 parts, so that they are off by 2^-14 at most (one part: 2^-7, more than the output's own
 // rounding).  For bf16 outputs the weights' two parts are transposed into the B operand once and multiplied by the keys' scales
 // there, two at a time: the first product is rounded, what that leaves is exact (8 x 8 bits less their upper 8) and goes into the
-// second one.  That is a quarter of the conversions and transposes.  fp32 outputs: scaled in fp32, group by group, off by 2^-16.
+// second one.  That is a quarter of the conversions and transposes.  For fp32 outputs they are scaled in fp32, group by group, and
+// all 24 bits of the products come in three parts.
 template <int D, bool kF32>
 __device__ __forceinline__ void kv4_values(uint32_t half, int tile, const Kv4Lane<D> &at, const float (&p)[4], bool partial, int keys,
                                            float (&acc)[D / 16][4])
@@ -306,16 +307,21 @@ __device__ __forceinline__ void kv4_values(uint32_t half, int tile, const Kv4Lan
 #pragma unroll
     for (int j = 0; j < NG; ++j) {
         const uint32_t sel = j & 1 ? 0x7632u : 0x5410u;
-        uint32_t b0, b1, b2, b3;
+        uint32_t b0, b1, b2, b3, b4 = 0u, b5 = 0u;
         if (kF32) {
             const float s0 = j & 1 ? bf16_hi(sa[j / 2]) : bf16_lo(sa[j / 2]);
             const float s1 = j & 1 ? bf16_hi(sb[j / 2]) : bf16_lo(sb[j / 2]);
-            const float w0 = p[0] * s0, w1 = p[1] * s0, w2 = p[2] * s1, w3 = p[3] * s1;
-            const uint32_t h0 = ptx::cvt_bf16x2(w0, w1), h1 = ptx::cvt_bf16x2(w2, w3);
-            b0 = transpose8(h0);
-            b1 = transpose8(h1);
-            b2 = transpose8(ptx::cvt_bf16x2(w0 - bf16_lo(h0), w1 - bf16_hi(h0)));  // what the rounding left
-            b3 = transpose8(ptx::cvt_bf16x2(w2 - bf16_lo(h1), w3 - bf16_hi(h1)));
+            auto parts = [](float x, float y, uint32_t &first, uint32_t &second, uint32_t &third) {  // each what the roundings before it left
+                first = ptx::cvt_bf16x2(x, y);
+                x -= bf16_lo(first);
+                y -= bf16_hi(first);
+                second = ptx::cvt_bf16x2(x, y);
+                third = transpose8(ptx::cvt_bf16x2(x - bf16_lo(second), y - bf16_hi(second)));
+                first = transpose8(first);
+                second = transpose8(second);
+            };
+            parts(p[0] * s0, p[1] * s0, b0, b2, b4);
+            parts(p[2] * s1, p[3] * s1, b1, b3, b5);
         } else {
             const uint32_t s0 = __byte_perm(sa[j / 2], sb[j / 2], sel), s1 = __byte_perm(sc[j / 2], sd[j / 2], sel);
             b0 = bf2_mul(t0, s0);
@@ -329,6 +335,7 @@ __device__ __forceinline__ void kv4_values(uint32_t half, int tile, const Kv4Lan
             const uint32_t a0 = nib_bf16(x), a1 = nib_bf16(x >> 4), a2 = nib_bf16(y), a3 = nib_bf16(y >> 4);
             mma_b16(acc[2 * j + h], a0, a1, a2, a3, b0, b1);
             mma_b16(acc[2 * j + h], a0, a1, a2, a3, b2, b3);
+            if (kF32) mma_b16(acc[2 * j + h], a0, a1, a2, a3, b4, b5);
         }
     }
 }

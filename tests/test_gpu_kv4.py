@@ -310,6 +310,29 @@ def test_decode_kv4_weights_lose_less_than_the_output(pa, oracle, pa_env, hq, hk
 
 
 @pytest.mark.parametrize("env", [{}, {"PA_DECODE_PATH": "cluster", "PA_DECODE_CLUSTER": "3"}, {"PA_DECODE_PATH": "persist"}])
+@pytest.mark.parametrize("hq,hkv,d", [(16, 2, 128), (8, 1, 64)])
+def test_decode_kv4_weights_of_fp32_outputs(pa, pa_env, hq, hkv, d, env):
+    """Up to 16 keys and queries of one feature, so that hardly anything but the weights is rounded.  A logit x (in powers of two, below
+    2.2) is an exact product times a factor: off by 2^-22 x, its difference to what weights are relative to (below 16) by 2^-21, the
+    weight by 2^-22 more: 2^-22 (1 + ln 2 (2 + 2.2)) < 2^-20.  Its product with V's scale is rounded to 2^-24, and all of that is
+    summed: 16 terms of at most 2^-24 of the sum each lose 2^-20.  Twice all of it, for the sum of weights: 2^-18."""
+    pa_env(**env)
+    c = _Cache(pa, [2, 3, 4, 5, 7, 9, 12, 16, 11, 6], hkv, d, seed=29)
+    q = torch.zeros((10, hq, d))
+    q[:, torch.arange(hq), torch.arange(hq) * 4 % d] = 3.0
+    q = q.bfloat16().cuda()
+    o, lse, _ = pa.pa_decode_kv4(q, c.pool, c.table, c.lens_d, 5, 1, o_dtype=torch.float32, softmax_scale=0.125)
+    for b in range(10):
+        for h in range(hkv):
+            heads = slice(h * hq // hkv, (h + 1) * hq // hkv)
+            ref_o, ref_lse, size, most = plain.row_attention(q[b, heads].double(), c.k[b][:, h], c.v[b][:, h], 0.125)
+            assert float(most.max()) * 1.443 < 2.2
+            err = (o[b, heads].double() - ref_o).abs()
+            assert (err <= 2.0 ** -18 * size).all(), float((err / size).max() * 2 ** 18)
+            assert ((lse[b, heads].double() - ref_lse).abs() <= 2.0 ** -18).all()
+
+
+@pytest.mark.parametrize("env", [{}, {"PA_DECODE_PATH": "cluster", "PA_DECODE_CLUSTER": "3"}, {"PA_DECODE_PATH": "persist"}])
 @pytest.mark.parametrize("hq,hkv,d", [(14, 2, 128), (4, 1, 64)])
 def test_decode_kv4_values_near_the_largest(pa, oracle, pa_env, hq, hkv, d, env):
     """Values as large as their sum by the weights allows (its magnitudes stay below 3.02e38): finite, and right."""
