@@ -480,9 +480,10 @@ typedef struct {
 size_t pa_decode_kv4_workspace_bytes(const pa_kv4_params *p);
 
 /* As pa_decode_paged (the same row of the mask, block_table, cache_lens, outputs, and pa_decode_status on the
- * workspace), on a 4-bit pool.  Logits are sums of exact products in fp32.  The weights, times V's scales, are
- * held in two bf16 parts, for fp32 outputs in three.
- * Outputs are finite where the values' magnitudes, summed by the weights exp(S - max S), stay below fp32's largest.
+ * workspace), on a 4-bit pool.  Logits are sums in fp32 of products of the keys' integers with the queries, which each
+ * head's power of two brings into fp16: a feature of q is off by 2^-35 of the head's largest magnitude (or of 2^-100) at
+ * most, and exact from 2^-27 of it on.  The weights, times V's scales, are held in two bf16 parts, for fp32 outputs in
+ * three.  Outputs are finite where the logits are and the values' magnitudes, summed by exp(S - max S), stay below 3.3e38.
  * workspace: device, 16-byte aligned, >= pa_decode_kv4_workspace_bytes(p); calls that share one must not
  * overlap on the GPU.  A table entry outside [0, n_pages) is clamped into the pool; the sequence's result is
  * then meaningless.  Few rows (sequence and KV head) take a thread-block cluster each.  Many or long ones are

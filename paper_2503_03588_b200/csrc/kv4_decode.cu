@@ -8,7 +8,7 @@
 // V's scales folded into the weights: one 16-bit weight per key and group.
 //
 // Logits take fp16 operands: q is bf16, and each head is multiplied by a power of two so that its largest entry lies in [2^10, 2^11)
-// and fits (entries below 2^-24 of it lose bits).  Weights are bf16, since V's scales may differ by any factor from key to key
+// and fits (an entry is off by 2^-35 of the largest at most, which smaller entries than 2^-27 of it feel).  Weights are bf16, since V's scales may differ by any factor from key to key
 // and from group to group, in two parts (one would be off by as much as the output's own rounding), for fp32 outputs in three.
 //
 // The nibbles become 16-bit numbers without conversions.  K: w & 0x000f000f is two fp16 subnormals, u 2^-24, and w & 0x00f000f0 is
@@ -449,9 +449,10 @@ __device__ __forceinline__ float natural(float m, float l) { return (m + log2f(l
 // blocks at a time, 16 keys each and all features, with maximum, sum and output of their own, and a warp that fetches the
 // blocks into a ring of stages.  The eight results are merged through shared memory and pushed to the CTA that merges a
 // head (CTA h % R) by asynchronous stores that count their bytes on a barrier of that CTA.
-// Bound by the chain (cycles, one sequence of 4001 tokens, 4 rows of 7 blocks, a CTA each): length 600, page 1400, block landed
-// 2300, logits and values 4100, pushed 4600, received 5300, done 6000; 4.4 us a call.  Eight sequences of 64K to 128K tokens, 32
-// rows in clusters of 8: 6.2 us.
+// Bound by the chain (cycles, one sequence of 4001 tokens, 4 rows of 9 blocks in clusters of 8; logits and values are some 100 more
+// since the weights come in two parts): length 600, page 1400, block landed 2300, logits and values 4100, pushed 4600, received
+// 5300, done 6000; 4.5 us a call.  Eight sequences of 64K to 128K tokens, 32 rows in clusters of 8: 6.5 us.  24 sequences of 64
+// features, rows of up to 45 blocks in clusters of 2, fp32 outputs: 15.2 us.
 // ------------------------------------------------------------------------------------------
 constexpr int kC4Consumers = 8;
 constexpr int kC4Threads = 32 * (kC4Consumers + 1);
@@ -688,9 +689,10 @@ __global__ void __launch_bounds__(kC4Threads, 2) kv4_cluster_kernel(const Kv4Arg
 // Where no row is long, ranges are rounded to whole rows instead, and nothing is left for the second kernel.
 // The ranges follow from the lengths, which are on the device: each CTA sums all sequences' blocks up (a thread takes
 // batch / 384 of them), and each thread looks one block of the CTA's range up.
-// Bound by instructions: a block of 64 keys, 128 features and up to eight heads takes about 1250, and the pipe of masks,
-// shifts and byte permutations is 60 % busy.  256 sequences of 4K to 16K tokens, 1024 rows, 99.5 MB: 31.5 us, 3.2 TB/s.  Of these the
-// blocks take 21, the start 2.7, a CTA's wait for its last warp 2.3, the merge 2.4, unequal shares of whole rows 3.
+// Bound by instructions: a block of 64 keys, 128 features and up to eight heads takes about 1500 (260 of them for the weights' second
+// part), half of the issue slots, and the pipe of masks, shifts and byte permutations is 40 % busy.  256 sequences of 4K to 16K
+// tokens, 1024 rows, 99.5 MB: 34.5 us, 2.9 TB/s.  Of these the blocks take 24, the start 2.7, a CTA's wait for its last warp 2.3,
+// the merge 2.4, unequal shares of whole rows 3.
 // ------------------------------------------------------------------------------------------
 constexpr int kR4Warps = 12;
 constexpr int kR4Threads = 32 * kR4Warps;
@@ -1266,8 +1268,10 @@ extern "C" pa_status pa_decode_kv4(const pa_kv4_params *p, const void *q, const 
     const int64_t rows = (int64_t)a.batch * a.Hkv;
     // A cluster per row, as many CTAs as run all at once (two per SM), where that is faster than ranges.  Measured with 128 features,
     // G = 7 (us): a cluster's CTA takes 4 + 0.72 per block, ranges take 14 + 0.26 per block of an SM's share, 9 where they are of
-    // whole rows; with 64 features all of it times 0.6.  Rows of 102 blocks: 144 rows 41 and 43, 192 rows (one CTA each, which
-    // leaves a third of the places empty) 75 and 51; rows of 11 blocks: 192 rows 12.3 and 18.5, 296 rows 12.6 and 13.5.
+    // whole rows; with 64 features all of it times 0.6.  Clusters and ranges, rows of 95 blocks: 144 rows 41.2 and 43.1 (ranges are
+    // taken), 192 rows (one CTA each, which leaves a third of the places empty) 75.8 and 54.0; rows of 46 blocks: 96 rows 20.8 and
+    // 22.1, 192 rows 37.5 and 31.0, 296 rows 38.9 and 36.6 (clusters are taken); rows of 11 blocks: 192 rows 12.1 and 18.7, 296 rows
+    // 12.6 and 13.3.  64 features: rows of 46 blocks, 96 rows 13.7 and 17.7, 192 rows 23.6 and 22.4, 296 rows 23.9 and 25.6.
     int R = 0;
     auto stages_of = [&](int r) {
         // (Each four warps wait for every other block: if stages are used again their number is even, so that a stage is

@@ -7,9 +7,9 @@
 // Bound by memory: a head is read and written once (backward: the head, its output's gradient, its gradient).  D / 8 or D / 16 lanes
 // share a head, each with pairs that belong together under the rotation, so that nothing but the norm's sums crosses lanes;
 // arithmetic goes two numbers an instruction, and what a token's heads share stays in registers.
-// Measured, 28 and 4 heads of 128 features, 32768 tokens: forward 90 us (554 MB, 0.94 of a copy's rate), backward with fp32
-// gradients 172 us (1074 MB, 0.95); 8 tokens forward 2.0 us; 4505 tokens of 16 and 4 heads of 64 features forward 8.2 us, backward
-// 10.9 us (two kernels).
+// Measured in a graph, 28 and 4 heads of 128 features, 32768 tokens: forward 90 us (554 MB, 0.94 of a copy's rate), backward with fp32
+// gradients 172 us (1074 MB, 0.95); 8 tokens forward 2.0 us; 3406 tokens of 16 and 4 heads of 64 features forward 8.2 us, backward
+// 11.1 us (two kernels).
 #include <cuda_bf16.h>
 #include <math.h>
 
@@ -642,7 +642,8 @@ static int64_t backward_parts(const pa_rope_params *p)
 }
 // Up to this many warps of one piece each, else the persistent ones that ring.  Measured (us, one piece a warp and persistent):
 // 28 and 4 heads of 128 features, 600 tokens 4.6 and 6.5, 1200 tokens 7.5 and 7.3, 2500 tokens 14.1 and 10.6; 16 and 4 heads of
-// 64, 1200 tokens 3.4 and 4.5, 3500 tokens 6.8 and 7.5, 4736 tokens 8.7 and 7.6.
+// 64, 1200 tokens 3.4 and 4.5, 3500 tokens (17500 warps) 6.8 and 7.5, 4736 tokens 8.7 and 7.6.  The two cross near 18000 warps with 128
+// features and near 20000 with 64; from the line to there the persistent form is up to a tenth the slower one.
 constexpr int64_t kRopeFewWarps = 148 * 112;
 
 }  // namespace pa

@@ -7,9 +7,10 @@
 // Bound by latency: a launch, the sums, then a chain from a token's sequence over its page to its slot.  Up to 1024 sequences every
 // CTA takes the sums itself, which costs less than a kernel that has to wait for them.  A warp finds the sequences of its first and
 // last token 32 at a time, and a lane the one of its own between them; a lane's pages are all on their way before it writes.
-// Measured: a decoding step of 64 sequences 2.2 us; 500 prompts of up to 4000 tokens, 0.98 million in all, 7.9 us (sums and
-// launch 3.6 of them; 12 bytes a token are written at 2.7 TB/s; in two kernels 10.8; with one set of four tokens a lane 11.2, and
-// with four sets 9.4).
+// Measured: a decoding step of 64 sequences 2.2 us; 500 prompts of up to 4000 tokens, 1.15 million in all, 8.0 us (sums and
+// launch 3.6 of them; 12 bytes a token are written at 3.1 TB/s; in two kernels 10.8; with one set of four tokens a lane 11.2, and
+// with four sets 9.4).  500 prompts of 2294 tokens with results in place, a second kernel: 15.5 (7.4 without).  2500 sequences of a
+// token each, the sums by one CTA: 19.4; of 400 tokens each 17.7.
 #include <limits.h>
 
 #include "common.cuh"
