@@ -8,8 +8,9 @@
 // V's scales folded into the weights: one 16-bit weight per key and group.
 //
 // Logits take fp16 operands: q is bf16, and each head is multiplied by a power of two so that its largest entry lies in [2^10, 2^11)
-// and fits (an entry is off by 2^-35 of the largest at most, which smaller entries than 2^-27 of it feel).  Weights are bf16, since V's scales may differ by any factor from key to key
-// and from group to group, in two parts (one would be off by as much as the output's own rounding), for fp32 outputs in three.
+// and fits (an entry is off by 2^-35 of the largest at most, which smaller entries than 2^-27 of it feel).  Weights are bf16,
+// since V's scales may differ by any factor from key to key and from group to group, in two parts (one would be off by as much
+// as the output's own rounding), for fp32 outputs in three.
 //
 // The nibbles become 16-bit numbers without conversions.  K: w & 0x000f000f is two fp16 subnormals, u 2^-24, and w & 0x00f000f0 is
 // 16 times as much, for which the queries of the former are multiplied by 16; -8 sum_i q_i is what the accumulator starts
